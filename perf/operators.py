@@ -238,22 +238,26 @@ def prepare(case, seed):
         s["C"] = torch.empty(case["m"], case["n"], dtype=TYPES[case["out"]], device="cuda")
         if own:
             import paper_2503_01253_amd as nm
-            s["packed"] = nm.nmspmm_half_pack(s["Bc"], s["idx"], *shape[1:])
-            size = nm.nmspmm_half_workspace_bytes(*shape)
+            s["weight"] = nm.nmspmm_half_pack(s["Bc"], s["idx"], *shape[1:])
+            size = nm.nmspmm_half_workspace_bytes(case["m"], s["weight"])
             s["workspace"] = torch.empty(size, dtype=torch.uint8, device="cuda") if size > 0 else None
         else:
             s["B"] = _dense(s, case, TYPES[case["dtype"]])
     elif case["op"] == "append":
         s = _append_inputs(case, seed)
         s["q_out"] = torch.empty(s["q"].shape, dtype=s["q"].dtype, device="cuda")
+        if own:
+            import paper_2503_01253_amd as nm
+            s["cache"] = nm.nmspmm_kv_cache(s["k_pages"], s["v_pages"], s["table"])
     else:
         s = _attend_inputs(case, seed)
         s["out"] = torch.empty_like(s["q"])
         s["longest"] = case["length"]
         if own:
             import paper_2503_01253_amd as nm
-            size = nm.nmspmm_kv_attend_workspace_bytes(case["batch"], case["heads"] * case["group"], case["heads"],
-                                                       case["dim"], case["length"], case["window"])
+            s["cache"] = nm.nmspmm_kv_cache(s["k_pages"], s["v_pages"], s["table"])
+            size = nm.nmspmm_kv_attend_workspace_bytes(s["cache"], case["heads"] * case["group"], case["length"],
+                                                       window=case["window"])
             s["workspace"] = torch.empty(size, dtype=torch.uint8, device="cuda") if size > 0 else None
     s["case"] = dict(case)
     return s
@@ -298,19 +302,16 @@ def _rotate(x, cos, sin, interleaved):
 def _run_product(s, case):
     if own:
         import paper_2503_01253_amd as nm
-        return nm.nmspmm_half_run(s["A"], s["packed"], s["C"],
-                                  *(case[x] for x in ("m", "n", "k", "N", "M", "V")), alpha=case["M"] / case["N"],
-                                  bias=s["bias"], act=case["act"], mul=s["mul"], residual=s["residual"],
-                                  workspace=s["workspace"])
+        return nm.nmspmm_half_run(s["A"], s["weight"], s["C"], alpha=case["M"] / case["N"], bias=s["bias"],
+                                  act=case["act"], mul=s["mul"], residual=s["residual"], workspace=s["workspace"])
     return _epilogue(s, case, s["A"].float() @ s["B"].float(), torch.float32).to(s["C"].dtype)
 
 
 def _run_append(s, case):
     if own:
         import paper_2503_01253_amd as nm
-        nm.nmspmm_kv_append(s["k"], s["v"], s["k_pages"], s["v_pages"], s["table"], s["seq"], s["pos"],
-                            cos=s["cos"], sin=s["sin"], q=s["q"], q_out=s["q_out"],
-                            interleaved=case["interleaved"])
+        nm.nmspmm_kv_append(s["cache"], s["k"], s["v"], s["seq"], s["pos"], cos=s["cos"], sin=s["sin"], q=s["q"],
+                            q_out=s["q_out"], interleaved=case["interleaved"])
         return s["k_pages"], s["v_pages"], s["q_out"]
     pos = s["pos"].long()
     page, slot = s["table"][s["seq"].long(), pos // case["page"]].long(), pos % case["page"]
@@ -328,9 +329,8 @@ def _run_append(s, case):
 def _run_attend(s, case):
     if own:
         import paper_2503_01253_amd as nm
-        return nm.nmspmm_kv_attend(s["q"], s["k_pages"], s["v_pages"], s["table"], s["lengths"], s["out"],
-                                   scale=case["dim"] ** -0.5, window=case["window"], max_length=s["longest"],
-                                   workspace=s["workspace"])
+        return nm.nmspmm_kv_attend(s["cache"], s["q"], s["lengths"], s["out"], scale=case["dim"] ** -0.5,
+                                   window=case["window"], max_length=s["longest"], workspace=s["workspace"])
     B, H, G, D, S, window = (case[x] for x in ("batch", "heads", "group", "dim", "page", "window"))
     out = torch.empty(B, H, G, D, device="cuda")
     lengths = s["lengths"].long()
