@@ -12,3 +12,8 @@ from .binding import (  # noqa: F401
     nmspmm_kernel_name, nmspmm_kernel_name_ws, nmspmm_run, nmspmm_run_ex, nmspmm_run_noalloc, nmspmm_run_ptr, nmspmm_run_ws,
     nmspmm_status_string, nmspmm_validate_idx, nmspmm_workspace_bytes,
 )
+from .serve import (  # noqa: F401
+    HALF_ACTS, NMSPMM_BF16, NMSPMM_F16, NMSPMM_F32, SERVE_EXPORTS, HalfWeight, KvCache,
+    nmspmm_half_bytes, nmspmm_half_kernel_name, nmspmm_half_pack, nmspmm_half_run, nmspmm_half_workspace_bytes,
+    nmspmm_kv_append, nmspmm_kv_attend, nmspmm_kv_attend_workspace_bytes, nmspmm_kv_cache,
+)

@@ -1,0 +1,46 @@
+// Shared by the units of the 16-bit product: the epilogue (device code).
+#ifndef NMSPMM_HALF_H
+#define NMSPMM_HALF_H
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "nmspmm_dtype.h"
+#include "nmspmm_serve.h"
+
+namespace nmspmm {
+
+// C[i][j] = act(alpha * sum + bias[j]) * mul[i][j] + residual[i][j], in fp32,
+// rounded once.  mul and residual have C's type.
+struct HalfEpilogue {
+    void *C;
+    const float *bias;
+    const void *mul, *residual;
+    int64_t ldc, ld_mul, ld_residual;
+    float alpha;
+    int act;
+};
+
+__device__ __forceinline__ float half_act(float y, int act)
+{
+    if (act == NMSPMM_HALF_ACT_RELU) return y < 0.f ? 0.f : y;      // NaN stays NaN
+    if (act == NMSPMM_HALF_ACT_GELU) return 0.5f * y * (1.f + erff(y * 0.70710678118f));
+    if (act == NMSPMM_HALF_ACT_SILU) return y / (1.f + __expf(-y));
+    return y;
+}
+
+template <class O>
+__device__ __forceinline__ void half_store(const HalfEpilogue &e, int64_t i, int64_t j, float sum)
+{
+    float y = e.alpha * sum;
+    if (e.bias) y += e.bias[j];
+    y = half_act(y, e.act);
+    if (e.mul) y *= to_f32(static_cast<const O *>(e.mul)[i * e.ld_mul + j]);
+    if (e.residual) y += to_f32(static_cast<const O *>(e.residual)[i * e.ld_residual + j]);
+    static_cast<O *>(e.C)[i * e.ldc + j] = from_f32<O>(y);
+}
+
+}  // namespace nmspmm
+
+#endif

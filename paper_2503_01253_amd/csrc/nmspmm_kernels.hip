@@ -26,6 +26,7 @@
 #include "nmspmm_stream.h"
 #include "nmspmm_tiled.h"
 #include "nmspmm_tiles.h"
+#include "nmspmm_workspace.h"
 
 namespace nmspmm {
 namespace {
@@ -1244,7 +1245,8 @@ nmspmm_status_t check_run_args(const float *A, const float *Bc, const uint8_t *i
     return NMSPMM_OK;
 }
 
-// Workspaces of the calls that bring none (nmspmm_run, nmspmm_run_ex): one
+// Workspaces of the calls that bring none (nmspmm_run, nmspmm_run_ex, and
+// through nmspmm_workspace.h the entry points of nmspmm_serve.h): one
 // buffer per (device, stream), allocated on the first call that needs it
 // (and again, larger, when a call needs more) and kept for the next calls on
 // that stream.  Each call makes its stream wait for the event the buffer's
@@ -1283,9 +1285,8 @@ void ws_drop(WsEntry &e)
     e = WsEntry{};
 }
 
-// A workspace of at least `need` bytes for a call on `stream` (the current
-// device), ordered after the buffer's previous use; null when none can be
-// had.  ws_done(...) must follow the call's launches.
+}  // namespace
+
 void *ws_acquire(hipStream_t stream, size_t need, int *slot)
 {
     int dev = -1;
@@ -1342,7 +1343,6 @@ void *ws_acquire(hipStream_t stream, size_t need, int *slot)
     return e.buf;
 }
 
-// After the call's launches on `stream`: mark the buffer's last use.
 hipError_t ws_done(int slot, hipStream_t stream)
 {
     std::lock_guard<std::mutex> lock(g_ws_mu);
@@ -1350,8 +1350,6 @@ hipError_t ws_done(int slot, hipStream_t stream)
     return hipEventRecord(g_ws[slot].done, stream);
 }
 
-// Whether work on `stream` is being captured into a graph (or that cannot be
-// told): such calls take no cached workspace.
 bool capturing(hipStream_t stream)
 {
     hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
@@ -1361,6 +1359,8 @@ bool capturing(hipStream_t stream)
     }
     return cs != hipStreamCaptureStatusNone;
 }
+
+namespace {
 
 // `pooled`: a call whose workspace (if any) is smaller than its workspace
 // plan needs takes the stream's cached workspace instead, outside graph

@@ -1,0 +1,329 @@
+"""ctypes binding of the decoding-step operators (include/nmspmm_serve.h): the
+16-bit N:M product and the paged key-value cache, under the C names.
+
+Argument marshalling only, as in binding.py: every step runs in the library's
+HIP kernels, and there is no fallback.  A packed weight (``HalfWeight``) and a
+cache (``KvCache``) are handles that a program makes once and passes to every
+call; they hold the tensors and their description, nothing of a call.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import binding
+from .binding import _call, _check, _raw_stream
+
+NMSPMM_F32, NMSPMM_BF16, NMSPMM_F16 = 0, 1, 2
+HALF_ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+SERVE_EXPORTS = (
+    "nmspmm_half_bytes", "nmspmm_half_pack", "nmspmm_half_workspace_bytes", "nmspmm_half_run",
+    "nmspmm_half_kernel_name", "nmspmm_kv_append", "nmspmm_kv_attend_workspace_bytes", "nmspmm_kv_attend",
+)
+
+
+class _Weight(ctypes.Structure):
+    _fields_ = [("packed", ctypes.c_void_p), ("dtype", ctypes.c_int), ("N", ctypes.c_int32), ("M", ctypes.c_int32),
+                ("V", ctypes.c_int32), ("k", ctypes.c_int64), ("n", ctypes.c_int64)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 3),
+                ("v_stride", ctypes.c_int64 * 3), ("pages", ctypes.c_int64), ("table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("sequences", ctypes.c_int64), ("table_pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int)]
+
+
+_Pair = ctypes.c_int64 * 2
+_lib = None
+_dtypes = None
+
+
+def _library():
+    """The library with this header's signatures declared."""
+    global _lib, _dtypes
+    if _lib is None:
+        import torch
+        L = binding.lib()
+        declare(L)
+        _dtypes = {torch.float32: NMSPMM_F32, torch.bfloat16: NMSPMM_BF16, torch.float16: NMSPMM_F16}
+        _lib = L
+    return _lib
+
+
+def declare(L):
+    """Declares the signatures of nmspmm_serve.h on a handle of the library."""
+    I64, I, P, F, Z = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_float, ctypes.c_size_t
+    W, C = ctypes.POINTER(_Weight), ctypes.POINTER(_Cache)
+    S = ctypes.POINTER(ctypes.c_int64)
+    L.nmspmm_half_bytes.argtypes = [I64, I64, I, I, I]
+    L.nmspmm_half_bytes.restype = I64
+    L.nmspmm_half_pack.argtypes = [P, I, P, W, P]
+    L.nmspmm_half_pack.restype = I
+    L.nmspmm_half_workspace_bytes.argtypes = [I64, W]
+    L.nmspmm_half_workspace_bytes.restype = I64
+    L.nmspmm_half_kernel_name.argtypes = [I64, W, I]
+    L.nmspmm_half_kernel_name.restype = ctypes.c_char_p
+    L.nmspmm_half_run.argtypes = [P, I64, W, P, I64, I, I64, F, P, I, P, I64, P, I64, P, Z, P]
+    L.nmspmm_half_run.restype = I
+    L.nmspmm_kv_append.argtypes = [C, P, S, P, S, I, I64, P, P, P, P, I64, I, I, P, S, P, S, I64, P]
+    L.nmspmm_kv_append.restype = I
+    L.nmspmm_kv_attend_workspace_bytes.argtypes = [C, I64, I64, I64]
+    L.nmspmm_kv_attend_workspace_bytes.restype = I64
+    L.nmspmm_kv_attend.argtypes = [C, P, S, I, I64, P, I64, I64, F, P, S, P, P, Z, P]
+    L.nmspmm_kv_attend.restype = I
+    return L
+
+
+def _require(name, t, dtypes, dim, device):
+    """A tensor of one of `dtypes` with `dim` dimensions on `device` (None:
+    any CUDA device), its last dimension contiguous."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor of {' or '.join(str(d) for d in dtypes)}")
+    if t.dim() != dim:
+        raise ValueError(f"{name} must be {dim}-D")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, {device} expected")
+
+
+def _shape(name, t, shape):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def _workspace(t, device):
+    """Address and size of a workspace tensor, or nothing."""
+    if t is None:
+        return None, 0
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous():
+        raise TypeError("workspace must be a contiguous CUDA tensor of torch.uint8")
+    if t.device != device:
+        raise ValueError(f"workspace is on {t.device}, {device} expected")
+    return t.data_ptr(), t.numel()
+
+
+class HalfWeight:
+    """An N:M sparse weight laid out by nmspmm_half_pack for nmspmm_half_run."""
+
+    def __init__(self, packed, dtype, k, n, N, M, V):
+        _library()
+        if dtype not in _dtypes:
+            raise TypeError(f"dtype must be torch.bfloat16 or torch.float16, not {dtype}")
+        self.packed, self.dtype, self.device = packed, dtype, packed.device
+        self.k, self.n, self.N, self.M, self.V = k, n, N, M, V
+        self._c = _Weight(packed.data_ptr(), _dtypes[dtype], N, M, V, k, n)
+        self._ref = ctypes.pointer(self._c)
+
+
+def nmspmm_half_bytes(k: int, n: int, N: int, M: int, V: int) -> int:
+    return int(_library().nmspmm_half_bytes(k, n, N, M, V))
+
+
+def nmspmm_half_pack(Bc, idx, n: int, k: int, N: int, M: int, V: int, dtype=None, packed=None, stream=None):
+    """Lays Bc (w x n, fp32 or 16-bit) and idx (w x q uint8), contiguous CUDA
+    tensors as nmspmm_compress_device writes them, out for nmspmm_half_run and
+    returns the ``HalfWeight``.  ``dtype`` is the weight's type (default: Bc's,
+    bfloat16 for an fp32 Bc).  ``packed``: the uint8 tensor to write,
+    nmspmm_half_bytes long (default: a new one)."""
+    import torch
+    L = _library()
+    size = nmspmm_half_bytes(k, n, N, M, V)
+    if size < 0:
+        raise binding.NmSpmmError("nmspmm_half_pack", binding.NMSPMM_ERR_INVALID_ARG,
+                                  f"invalid shape k={k} n={n} N={N} M={M} V={V}")
+    for name, t, dtypes, numel in (("Bc", Bc, tuple(_dtypes), (k // M) * N * n),
+                                   ("idx", idx, (torch.uint8,), (k // M) * N * (n // V))):
+        if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or not t.is_cuda or not t.is_contiguous():
+            raise TypeError(f"{name} must be a contiguous CUDA tensor of {' or '.join(str(d) for d in dtypes)}")
+        if t.device != Bc.device:
+            raise ValueError(f"{name} is on {t.device}, {Bc.device} expected")
+        if t.numel() != numel:
+            raise ValueError(f"{name} has {t.numel()} elements, expected {numel}")
+    if dtype is None:
+        dtype = torch.bfloat16 if Bc.dtype == torch.float32 else Bc.dtype
+    at = Bc.get_device()
+    if packed is None:
+        packed = torch.empty(size, dtype=torch.uint8, device=Bc.device)
+        if stream is not None:
+            packed.record_stream(stream)
+    elif _workspace(packed, Bc.device)[1] < size:
+        raise ValueError(f"packed has {packed.numel()} bytes, {size} needed")
+    weight = HalfWeight(packed, dtype, k, n, N, M, V)
+    st = _call(torch, at, L.nmspmm_half_pack, Bc.data_ptr(), _dtypes[Bc.dtype], idx.data_ptr(), weight._ref,
+               _raw_stream(torch, at, stream))
+    _check("nmspmm_half_pack", st)
+    return weight
+
+
+def nmspmm_half_workspace_bytes(m: int, weight: HalfWeight) -> int:
+    """Workspace bytes with which nmspmm_half_run splits k for m rows (0: it does not; -1: bad shape)."""
+    return int(_library().nmspmm_half_workspace_bytes(m, weight._ref))
+
+
+def nmspmm_half_kernel_name(m: int, weight: HalfWeight, with_workspace: bool = True) -> str:
+    return _library().nmspmm_half_kernel_name(m, weight._ref, int(with_workspace)).decode()
+
+
+def nmspmm_half_run(A, weight: HalfWeight, C, alpha: float = 1.0, bias=None, act: str = "none", mul=None,
+                    residual=None, workspace=None, stream=None):
+    """C = act(alpha * (A * B) + bias) * mul + residual on the GPU,
+    asynchronously on ``stream`` (default: torch's current stream).  A (m x k)
+    has the weight's type; C (m x n) that type or fp32; mul and residual C's
+    shape and type (either may be C itself); bias is n contiguous fp32 values.  Rows of A, C, mul
+    and residual may lie any stride apart.  act: "none", "relu", "gelu" or
+    "silu".  ``workspace``: a contiguous uint8 tensor, 256-byte aligned, of
+    nmspmm_half_workspace_bytes bytes (or None: the library's own)."""
+    import torch
+    L = _lib or _library()
+    dev = weight.device
+    _require("A", A, (weight.dtype,), 2, dev)
+    m = A.shape[0]
+    _shape("A", A, (m, weight.k))
+    _require("C", C, (weight.dtype, torch.float32), 2, dev)
+    _shape("C", C, (m, weight.n))
+    args = []
+    for name, t in (("mul", mul), ("residual", residual)):
+        if t is None:
+            args += [None, 0]
+        else:
+            _require(name, t, (C.dtype,), 2, dev)
+            _shape(name, t, C.shape)
+            args += [t.data_ptr(), t.stride(0)]
+    if bias is not None:
+        _require("bias", bias, (torch.float32,), 1, dev)
+        _shape("bias", bias, (weight.n,))
+    if act not in HALF_ACTS:
+        raise ValueError(f"act must be one of {sorted(HALF_ACTS)}")
+    at = C.get_device()
+    st = _call(torch, at, L.nmspmm_half_run, A.data_ptr(), A.stride(0), weight._ref, C.data_ptr(), C.stride(0),
+               _dtypes[C.dtype], m, alpha, None if bias is None else bias.data_ptr(), HALF_ACTS[act], *args,
+               *_workspace(workspace, dev), _raw_stream(torch, at, stream))
+    if st:
+        _check("nmspmm_half_run", st)
+    return C
+
+
+class KvCache:
+    """A paged key-value cache: k_pages and v_pages (pages, page_size, heads,
+    dim), any strides with a contiguous last dimension, and the table
+    (sequences, table_pages) of int32 page numbers.  The tensors stay the
+    caller's: their contents, the table's among them, are read on the device
+    by every call."""
+
+    def __init__(self, k_pages, v_pages, table):
+        import torch
+        _library()
+        _require("k_pages", k_pages, tuple(_dtypes), 4, None)
+        _require("v_pages", v_pages, (k_pages.dtype,), 4, k_pages.device)
+        _shape("v_pages", v_pages, k_pages.shape)
+        _require("table", table, (torch.int32,), 2, k_pages.device)
+        self.k_pages, self.v_pages, self.table = k_pages, v_pages, table
+        self.device, self.dtype = k_pages.device, k_pages.dtype
+        self.pages, self.page_size, self.heads, self.dim = k_pages.shape
+        self.sequences, self.table_pages = table.shape
+        S = ctypes.c_int64 * 3
+        self._c = _Cache(k_pages.data_ptr(), v_pages.data_ptr(), S(*k_pages.stride()[:3]), S(*v_pages.stride()[:3]),
+                         self.pages, table.data_ptr(), table.stride(0), self.sequences, self.table_pages,
+                         self.page_size, self.heads, self.dim, _dtypes[k_pages.dtype])
+        self._ref = ctypes.pointer(self._c)
+
+
+def nmspmm_kv_cache(k_pages, v_pages, table) -> KvCache:
+    """The handle of a paged cache, for the calls below."""
+    return KvCache(k_pages, v_pages, table)
+
+
+def nmspmm_kv_append(cache: KvCache, k, v, seq, pos, cos=None, sin=None, q=None, q_out=None, interleaved=False,
+                     stream=None):
+    """Writes k and v (tokens, heads, dim) of new tokens into the cache, token
+    t at position pos[t] of sequence seq[t] (int32), asynchronously on
+    ``stream``.  With cos and sin (positions, rot/2, contiguous fp32) the first
+    rot dimensions of k, and of q (tokens, q_heads, dim) into q_out (default:
+    in place), are turned by their position's angles, in pairs (d, d + rot/2)
+    or, ``interleaved``, (2d, 2d + 1).  k, v, q and q_out have one type; their
+    first two dimensions may have any strides.  Tokens without a place (a
+    negative position, say) are skipped.  Returns q_out."""
+    import torch
+    L = _lib or _library()
+    dev = cache.device
+    _require("k", k, tuple(_dtypes), 3, dev)
+    kinds = (k.dtype,)
+    tokens = k.shape[0]
+    _shape("k", k, (tokens, cache.heads, cache.dim))
+    _require("v", v, kinds, 3, dev)
+    _shape("v", v, k.shape)
+    for name, t in (("seq", seq), ("pos", pos)):
+        _require(name, t, (torch.int32,), 1, dev)
+        _shape(name, t, (tokens,))
+    angles = (None, None, 0, 0)
+    if cos is not None or sin is not None:
+        for name, t in (("cos", cos), ("sin", sin)):
+            _require(name, t, (torch.float32,), 2, dev)
+            _shape(name, t, cos.shape)
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        angles = (cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1])
+    queries = (None, None, None, None, 0)
+    if q is not None:
+        if q_out is None:
+            q_out = q
+        _require("q", q, kinds, 3, dev)
+        _shape("q", q, (tokens, q.shape[1], cache.dim))
+        _require("q_out", q_out, kinds, 3, dev)
+        _shape("q_out", q_out, q.shape)
+        queries = (q.data_ptr(), _Pair(*q.stride()[:2]), q_out.data_ptr(), _Pair(*q_out.stride()[:2]), q.shape[1])
+    at = k.get_device()
+    st = _call(torch, at, L.nmspmm_kv_append, cache._ref, k.data_ptr(), _Pair(*k.stride()[:2]), v.data_ptr(),
+               _Pair(*v.stride()[:2]), _dtypes[k.dtype], tokens, seq.data_ptr(), pos.data_ptr(), *angles,
+               int(interleaved), *queries, _raw_stream(torch, at, stream))
+    if st:
+        _check("nmspmm_kv_append", st)
+    return q_out
+
+
+def nmspmm_kv_attend_workspace_bytes(cache: KvCache, q_heads: int, max_length: int, window: int = 0) -> int:
+    """Workspace bytes with which nmspmm_kv_attend splits sequences (0: it does not; -1: bad sizes)."""
+    return int(_library().nmspmm_kv_attend_workspace_bytes(cache._ref, q_heads, max_length, window))
+
+
+def nmspmm_kv_attend(cache: KvCache, q, lengths, out, scale=None, window: int = 0, max_length=None, lse=None,
+                     workspace=None, stream=None):
+    """Attention of one new token per sequence over the cache, asynchronously
+    on ``stream``: q and out (sequences, q_heads, dim) of one type, any strides
+    in the first two dimensions; lengths (sequences,) int32, the new token
+    included.  ``scale``: default dim ** -0.5.  ``window`` > 0: the last
+    ``window`` positions only.  ``max_length``: an upper bound of the lengths
+    (default: what the table can hold); a tighter one splits the work better.
+    ``lse``: (sequences, q_heads) contiguous fp32 for the log-sum-exp, or None.
+    ``workspace``: as for nmspmm_half_run, nmspmm_kv_attend_workspace_bytes
+    bytes."""
+    import torch
+    L = _lib or _library()
+    dev = cache.device
+    _require("q", q, tuple(_dtypes), 3, dev)
+    _shape("q", q, (cache.sequences, q.shape[1], cache.dim))
+    _require("out", out, (q.dtype,), 3, dev)
+    _shape("out", out, q.shape)
+    _require("lengths", lengths, (torch.int32,), 1, dev)
+    _shape("lengths", lengths, (cache.sequences,))
+    if lse is not None:
+        _require("lse", lse, (torch.float32,), 2, dev)
+        _shape("lse", lse, q.shape[:2])
+        if not lse.is_contiguous():
+            raise ValueError("lse must be contiguous")
+    if max_length is None:
+        max_length = cache.table_pages * cache.page_size
+    if scale is None:
+        scale = cache.dim ** -0.5
+    at = q.get_device()
+    st = _call(torch, at, L.nmspmm_kv_attend, cache._ref, q.data_ptr(), _Pair(*q.stride()[:2]), _dtypes[q.dtype],
+               q.shape[1], lengths.data_ptr(), max_length, window, scale, out.data_ptr(), _Pair(*out.stride()[:2]),
+               None if lse is None else lse.data_ptr(), *_workspace(workspace, dev), _raw_stream(torch, at, stream))
+    if st:
+        _check("nmspmm_kv_attend", st)
+    return out

@@ -1,0 +1,367 @@
+"""The paged cache (nmspmm_kv_append, nmspmm_kv_attend) against plain fp64.
+
+Tolerances, derived.  Append: a turned value is two products and a sum in fp32,
+at most 3 * 2^-24 of |a| + |b| off, then one rounding u to the stored type
+(u = 2^-8 bf16, 2^-11 fp16 with 2^-25 absolute where subnormal, 2^-24 fp32);
+copies are exact.  Attend: a score is a dot product of dim terms and a scaling
+in fp32, off by at most es = (dim + 8) * 2^-24 * scale * sum |q||k|; a weight
+is then off by a factor of 1 +- (2 es + 2^-20) (its exponential and the
+denominator's), further by 2^-16 where weights meet 16-bit values in two 16-bit
+parts, and a sum of L terms by L * 2^-24; all this relative to sum w|v|.  The
+store rounds once by u of the result.
+"""
+import sys
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+import paper_2503_01253_amd as nm  # noqa: E402
+
+DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+ROUND = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 2.0 ** -24}
+
+
+def say(msg):
+    print(msg, file=sys.stderr, flush=True)
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def tensor(rng, shape, dtype):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(DTYPES[dtype]).cuda()
+
+
+def pages_of(shape, dtype, layout, fill=float("nan")):
+    """A pool of pages (pages, page, heads, dim) in one of several memory
+    orders."""
+    P, S, H, D = shape
+    new = lambda *s: torch.full(s, fill, dtype=DTYPES[dtype], device="cuda")  # noqa: E731
+    if layout == "plain":
+        return new(P, S, H, D)
+    if layout == "heads":       # every head's page contiguous
+        return new(P, H, S, D).permute(0, 2, 1, 3)
+    if layout == "padded":      # rows further apart than their length
+        return new(P, S, H, D + 8)[..., :D]
+    if layout == "odd":         # rows on no 16-byte boundary
+        return new(P, S, H, D + 1)[..., 1:]
+    if layout == "joint":       # keys and values of a token side by side
+        return new(P, S, 2, H, D)[:, :, 1]
+    raise ValueError(layout)
+
+
+# ---- append ----------------------------------------------------------------
+
+def turn64(x, cos, sin, rot, interleaved):
+    y, half = x.copy(), rot // 2
+    err = np.zeros_like(x)
+    for e in range(half):
+        i, j = (2 * e, 2 * e + 1) if interleaved else (e, e + half)
+        a, b = x[..., i], x[..., j]
+        c, s = cos[:, None, e], sin[:, None, e]
+        y[..., i], y[..., j] = a * c - b * s, a * s + b * c
+        err[..., i] = err[..., j] = 3 * 2.0 ** -24 * (np.abs(a) + np.abs(b))
+    return y, err
+
+
+def close(got, want, err, dtype, what):
+    tol = err * (1 + 2.0 ** -6) + np.abs(want) * ROUND[dtype] + (2.0 ** -25 if dtype == "f16" else 0)
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), f"{what}: {bad.sum()} off, worst {np.max(np.abs(got - want) - tol)}"
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f32", "bf16"), ("f16", "f16"), ("f32", "f32"),
+                                         ("f32", "f16"), ("bf16", "f32")])
+@pytest.mark.parametrize("tokens,heads,group,dim,page,rot,interleaved,layout", [
+    (1, 1, 1, 64, 16, 64, False, "plain"), (5, 2, 3, 128, 16, 128, False, "plain"), (64, 8, 4, 128, 16, 128, True, "plain"),
+    (70, 3, 2, 80, 7, 40, False, "heads"), (33, 2, 1, 96, 24, 96, True, "padded"), (9, 1, 2, 33, 5, 32, False, "odd"),
+    (17, 2, 0, 128, 1, 0, False, "joint"), (300, 2, 2, 64, 64, 64, False, "odd"), (12, 1, 1, 1, 3, 0, False, "plain"),
+    (11, 2, 2, 512, 16, 256, False, "plain"), (40, 2, 2, 40, 16, 24, True, "plain"), (21, 4, 1, 256, 32, 64, False, "joint"),
+    (8, 2, 2, 7, 4, 6, True, "plain"), (13, 2, 1, 24, 8, 4, False, "padded")])
+def test_append(tokens, heads, group, dim, page, rot, interleaved, layout, dtype, cache):
+    say(f"[append] {tokens} {heads}x{group} dim {dim} page {page} rot {rot} {interleaved} {layout} {dtype} {cache}")
+    rng = np.random.default_rng(tokens + dim)
+    sequences, wide = 4, 9
+    pages = sequences * wide + 2
+    kp, vp = (pages_of((pages, page, heads, dim), cache, layout, 3.0) for _ in range(2))
+    table = torch.from_numpy(rng.permutation(pages)[:sequences * wide].reshape(sequences, wide)).int().cuda()
+    tokens = min(tokens, sequences * wide * page)
+    places = rng.permutation(sequences * wide * page)[:tokens]
+    seq, pos = places // (wide * page), places % (wide * page)
+    # queries, keys and values in one row a token, keys and values side by side
+    qkv = tensor(rng, (tokens, group * heads + 2 * heads, dim), dtype)
+    q, k, v = qkv[:, :group * heads], qkv[:, group * heads::2], qkv[:, group * heads + 1::2]
+    half = rot // 2
+    cos = sin = None
+    if rot:
+        angle = rng.uniform(0, 6, (wide * page, half))
+        cos, sin = (torch.from_numpy(f(angle).astype(np.float32)).cuda() for f in (np.cos, np.sin))
+    c64, s64 = (f64(x)[pos] if rot else np.zeros((tokens, 0)) for x in (cos, sin))
+    q64, k64, v64 = f64(q), f64(k), f64(v)
+    cachehandle = nm.nmspmm_kv_cache(kp, vp, table)
+    q_out = torch.full((tokens, group * heads, dim + 2), 5.0, dtype=DTYPES[dtype], device="cuda")[..., :dim]
+    nm.nmspmm_kv_append(cachehandle, k, v, torch.from_numpy(seq).int().cuda(), torch.from_numpy(pos).int().cuda(),
+                        cos=cos, sin=sin, q=q if group else None, q_out=q_out if group else None,
+                        interleaved=interleaved)
+    torch.cuda.synchronize()
+    at = table.cpu().numpy()[seq, pos // page], pos % page
+    for pool, (want, err) in ((kp, turn64(k64, c64, s64, rot, interleaved)), (vp, (v64, 0 * v64))):
+        got = f64(pool)
+        close(got[at], want, err, cache, "written")
+        got[at] = 3.0
+        assert np.all(got == 3.0), "a slot that no token names was written"
+    if group:
+        want, err = turn64(q64, c64, s64, rot, interleaved)
+        close(f64(q_out), want, err, dtype, "queries")
+        nm.nmspmm_kv_append(cachehandle, k, v, torch.from_numpy(seq).int().cuda(), torch.from_numpy(pos).int().cuda(),
+                            cos=cos, sin=sin, q=q, interleaved=interleaved)       # in place
+        torch.cuda.synchronize()
+        assert torch.equal(q, q_out)
+
+
+def test_append_skips_tokens_without_a_place():
+    """Negative and too large positions and sequences, positions past the
+    angles, and table entries that name no page: nothing of such a token is
+    written, and the others' are."""
+    rng = np.random.default_rng(3)
+    heads, dim, page, wide, sequences, pages = 2, 64, 4, 3, 2, 6
+    kp, vp = (pages_of((pages, page, heads, dim), "bf16", "plain", 3.0) for _ in range(2))
+    table = torch.tensor([[0, 1, 99], [-1, 2, 3]], dtype=torch.int32).cuda()
+    seq = torch.tensor([0, 0, 2, -1, 1, 0, 0, 1, 1, 0], dtype=torch.int32).cuda()
+    pos = torch.tensor([-1, 12, 0, 0, 1, 9, 5, 4, 10, 2 ** 31 - 1], dtype=torch.int32).cuda()
+    written = {6: (1, 1), 7: (2, 0)}          # token 8 lies past the angles
+    tokens = len(seq)
+    k, v, q = (tensor(rng, (tokens, heads, dim), "bf16") for _ in range(3))
+    q_out = torch.full_like(q, 3.0)
+    angle = torch.zeros(10, 32).cuda()
+    nm.nmspmm_kv_append(nm.nmspmm_kv_cache(kp, vp, table), k, v, seq, pos, cos=angle.cos(), sin=angle.sin(), q=q,
+                        q_out=q_out)
+    torch.cuda.synchronize()
+    want_k, want_v, want_q = torch.full_like(kp, 3.0), torch.full_like(vp, 3.0), torch.full_like(q, 3.0)
+    for t, (pg, slot) in written.items():
+        want_k[pg, slot], want_v[pg, slot], want_q[t] = k[t], v[t], q[t]
+    assert torch.equal(kp, want_k) and torch.equal(vp, want_v) and torch.equal(q_out, want_q)
+
+
+# ---- attend ----------------------------------------------------------------
+
+def attend64(q, K, V, scale, weights16):
+    """One sequence's heads: q (heads, group, dim), K and V (L, heads, dim)."""
+    L, dim = K.shape[0], K.shape[2]
+    s = scale * np.einsum("hgd,lhd->hgl", q, K)
+    es = (dim + 8) * 2.0 ** -24 * abs(scale) * np.einsum("hgd,lhd->hgl", np.abs(q), np.abs(K)).max(-1, initial=0)
+    if L == 0:
+        return np.zeros_like(q), np.zeros_like(q), np.full(q.shape[:2], -np.inf)
+    top = s.max(-1, keepdims=True)
+    w = np.exp(s - top)
+    total = w.sum(-1, keepdims=True)
+    p = w / total
+    rel = 2 * es + 2.0 ** -20 + L * 2.0 ** -24 + (2.0 ** -16 if weights16 else 0)
+    return (np.einsum("hgl,lhd->hgd", p, V), rel[..., None] * np.einsum("hgl,lhd->hgd", p, np.abs(V)),
+            (np.log(total) + top)[..., 0])
+
+
+def run_attend(lengths, heads, group, dim, page, dtype, cache, layout="plain", window=0, scale=None, seed=0, spread=1.0,
+               workspace="library", max_length=None, wide=None):
+    rng = np.random.default_rng(seed + dim + sum(lengths))
+    B = len(lengths)
+    need = [-(-max(x, 0) // page) for x in lengths]
+    wide = wide or max(need + [1])
+    pages = sum(need) + 2
+    # what no sequence holds is NaN: it must not matter
+    kp, vp = (pages_of((pages, page, heads, dim), cache, layout) for _ in range(2))
+    table = torch.full((B, wide), 2 ** 30, dtype=torch.int32)
+    order = iter(rng.permutation(pages - 1) + 1)
+    K, V = [], []
+    for b, x in enumerate(lengths):
+        ids = [int(next(order)) for _ in range(need[b])]
+        table[b, :len(ids)] = torch.tensor(ids, dtype=torch.int32)
+        at = torch.tensor(ids, dtype=torch.long, device="cuda")
+        x = max(x, 0)
+        k, v = tensor(rng, (x, heads, dim), cache) * spread, tensor(rng, (x, heads, dim), cache)
+        where = torch.arange(x, device="cuda")
+        if x:
+            kp[at[where // page], where % page] = k
+            vp[at[where // page], where % page] = v
+        K.append(f64(k))
+        V.append(f64(v))
+    q = tensor(rng, (B, heads * group, dim), dtype)
+    out = torch.full((B, heads * group, dim + 3), 9.0, dtype=DTYPES[dtype], device="cuda")
+    lse = torch.full((B, heads * group), float("nan"), device="cuda")
+    handle = nm.nmspmm_kv_cache(kp, vp, table.cuda())
+    ws = None
+    if workspace == "caller":
+        size = nm.nmspmm_kv_attend_workspace_bytes(handle, heads * group, max_length or wide * page, window)
+        assert size >= 0
+        ws = torch.full((max(size, 1),), 255, dtype=torch.uint8, device="cuda")
+    nm.nmspmm_kv_attend(handle, q, torch.tensor(lengths, dtype=torch.int32).cuda(), out[..., :dim], scale=scale,
+                        window=window, max_length=max_length, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    assert torch.all(out[..., dim:] == 9.0)
+    got, got_lse, q64 = f64(out[..., :dim]), f64(lse), f64(q)
+    scale = dim ** -0.5 if scale is None else scale
+    for b, x in enumerate(lengths):
+        x = min(max(x, 0), wide * page, max_length if max_length is not None else x)
+        first = max(0, x - window) if window else 0
+        want, err, want_lse = attend64(q64[b].reshape(heads, group, dim), K[b][first:x], V[b][first:x], scale,
+                                       cache != "f32")
+        tol = err * (1 + 2.0 ** -6) + np.abs(want) * ROUND[dtype] + (2.0 ** -25 if dtype == "f16" else 0)
+        diff = np.abs(got[b].reshape(want.shape) - want)
+        assert np.all(diff <= tol), f"sequence {b} of length {x}: worst {np.max(diff / np.maximum(tol, 1e-300))}"
+        if x > first:
+            L = x - first
+            bound = np.abs(want_lse) * 2.0 ** -22 + (dim + 8) * 2.0 ** -24 * abs(scale) * np.einsum(
+                "hgd,lhd->hgl", np.abs(q64[b].reshape(heads, group, dim)), np.abs(K[b][first:x])).max(-1) + \
+                L * 2.0 ** -24 + 2.0 ** -20
+            assert np.all(np.abs(got_lse[b].reshape(want_lse.shape) - want_lse) <= bound)
+        else:
+            assert np.all(got_lse[b] == -np.inf) and np.all(got[b] == 0)
+    return handle, q, out
+
+
+LENGTHS = [0, 1, 2, 15, 16, 17, 31, 33, 64, 100, 129, 255, -3, 700]
+TYPES = [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"), ("f32", "bf16"), ("bf16", "f16")]
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("heads,group,dim,page,layout", [
+    (1, 1, 64, 16, "plain"), (8, 4, 128, 16, "plain"), (2, 8, 128, 16, "heads"), (4, 1, 64, 32, "padded"),
+    (2, 3, 80, 24, "plain"), (3, 7, 96, 1, "plain"), (1, 16, 128, 64, "joint"), (2, 5, 256, 16, "plain"),
+    (1, 2, 33, 7, "plain"), (2, 4, 128, 16, "odd"), (1, 20, 64, 16, "heads"), (1, 1, 512, 16, "plain"),
+    (1, 33, 128, 16, "plain"), (2, 2, 8, 3, "plain"), (1, 1, 1, 5, "plain"), (2, 2, 300, 9, "plain"),
+    (2, 16, 112, 48, "plain"), (1, 6, 192, 16, "plain"), (2, 8, 48, 16, "padded"), (1, 4, 16, 16, "plain")])
+def test_attend(heads, group, dim, page, layout, dtype, cache):
+    say(f"[attend] {heads}x{group} dim {dim} page {page} {layout} {dtype} {cache}")
+    run_attend(LENGTHS, heads, group, dim, page, dtype, cache, layout)
+
+
+@pytest.mark.parametrize("workspace", ["library", "caller"])
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("lengths,heads,group,dim,page", [
+    ([5000], 2, 4, 128, 16), ([4097, 3, 0, 2048], 1, 8, 64, 64), ([3000, 2999], 2, 1, 80, 24), ([9001], 1, 16, 128, 16)])
+def test_attend_split(lengths, heads, group, dim, page, dtype, cache, workspace):
+    say(f"[attend] split {lengths} {heads}x{group} dim {dim} page {page} {dtype} {cache} {workspace}")
+    run_attend(lengths, heads, group, dim, page, dtype, cache, workspace=workspace)
+
+
+@pytest.mark.parametrize("window", [1, 15, 64, 100, 1024, 10 ** 6])
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f32", "f32"), ("f32", "f16")])
+def test_attend_window(window, dtype, cache):
+    say(f"[attend] window {window} {dtype} {cache}")
+    run_attend([0, 1, 64, 65, 99, 101, 1500, 4096], 2, 4, 64, 16, dtype, cache, window=window)
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f16", "f16"), ("f32", "f32")])
+def test_attend_bounds_and_scales(dtype, cache):
+    """Lengths beyond max_length and beyond the table are cut; a scale of 0
+    averages, a negative one inverts; large scores (one position takes all)
+    neither overflow nor underflow into NaN."""
+    say(f"[attend] bounds {dtype} {cache}")
+    run_attend([10, 100, 300, 299], 2, 4, 64, 16, dtype, cache, max_length=100)
+    run_attend([0, 7, 300], 2, 4, 64, 16, dtype, cache, scale=0.0)
+    run_attend([1, 7, 300], 2, 4, 64, 16, dtype, cache, scale=-0.3)
+    run_attend([1, 40, 3000], 2, 4, 64, 16, dtype, cache, scale=4.0, spread=8.0)
+    run_attend([0, 0, 0], 2, 4, 64, 16, dtype, cache)
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("dim", [128, 33])
+def test_attend_leaves_out_pages_outside_the_cache(dim, dtype, cache):
+    """A table entry below 0 or past the cache's pages: its positions do not
+    count, as if the sequence did not hold them."""
+    rng = np.random.default_rng(5)
+    heads, group, page, pages = 2, 4, 16, 5
+    kp, vp = (tensor(rng, (pages, page, heads, dim), cache) for _ in range(2))
+    q = tensor(rng, (3, heads * group, dim), dtype)
+    full = torch.tensor([[4, -1, 2, 2 ** 31 - 1, 0], [-5, 7, 9, 5, -1], [1, 2, 3, 0, 4]], dtype=torch.int32).cuda()
+    near = torch.tensor([[4, 2, 0], [0, 0, 0], [1, 2, 3]], dtype=torch.int32).cuda()
+    out, want = torch.empty_like(q), torch.empty_like(q)
+    nm.nmspmm_kv_attend(nm.nmspmm_kv_cache(kp, vp, full), q, torch.tensor([70, 80, 48]).int().cuda(), out)
+    nm.nmspmm_kv_attend(nm.nmspmm_kv_cache(kp, vp, near), q, torch.tensor([38, 0, 48]).int().cuda(), want)
+    torch.cuda.synchronize()
+    assert torch.all(out[1] == 0)
+    tol = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -18       # two roundings; order of the sums
+    assert torch.all((out - want).abs() <= tol * (want.abs() + 1))
+
+
+@pytest.mark.parametrize("cache", ["bf16", "f32"])
+def test_offsets_past_32_bits(cache):
+    """Pages whose elements lie past 2^31: written, then read."""
+    say(f"[kv] far pages {cache}")
+    heads, dim, page, group = 8, 128, 16, 4
+    pages = 2 ** 31 // (heads * dim * page) + 40
+    kp, vp = (torch.empty(pages, page, heads, dim, dtype=DTYPES[cache], device="cuda") for _ in range(2))
+    rng = np.random.default_rng(1)
+    T = 40
+    ids = torch.tensor([[pages - 1, 0, pages - 7]], dtype=torch.int32).cuda()
+    handle = nm.nmspmm_kv_cache(kp, vp, ids)
+    k, v = (tensor(rng, (T, heads, dim), "f32") for _ in range(2))
+    nm.nmspmm_kv_append(handle, k, v, torch.zeros(T).int().cuda(), torch.arange(T).int().cuda())
+    at = ids[0].long()[torch.arange(T).cuda() // page], torch.arange(T).cuda() % page
+    torch.cuda.synchronize()
+    assert torch.equal(kp[at], k.to(kp.dtype)) and torch.equal(vp[at], v.to(vp.dtype))
+    q = tensor(rng, (1, heads * group, dim), cache)
+    out = torch.empty_like(q)
+    nm.nmspmm_kv_attend(handle, q, torch.tensor([T]).int().cuda(), out)
+    torch.cuda.synchronize()
+    want, err, _ = attend64(f64(q)[0].reshape(heads, group, dim), f64(kp[at]), f64(vp[at]), dim ** -0.5, cache != "f32")
+    assert np.all(np.abs(f64(out)[0].reshape(want.shape) - want) <= 1.02 * err + np.abs(want) * ROUND[cache])
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f32", "bf16")])
+def test_streams_graphs_and_determinism(dtype, cache):
+    """Append and attend on a stream of their own and replayed from a graph,
+    lengths growing between replays: the same bits as eager calls."""
+    say(f"[kv] graph {dtype} {cache}")
+    rng = np.random.default_rng(2)
+    heads, group, dim, page, B, wide = 2, 4, 128, 16, 3, 200
+    kp, vp = (tensor(rng, (B * wide, page, heads, dim), cache) for _ in range(2))
+    table = torch.arange(B * wide, dtype=torch.int32).view(B, wide).cuda()
+    handle = nm.nmspmm_kv_cache(kp, vp, table)
+    k, v = (tensor(rng, (B, heads, dim), dtype) for _ in range(2))
+    q = tensor(rng, (B, heads * group, dim), dtype)
+    angle = torch.rand(wide * page, dim // 2).cuda()
+    cos, sin = angle.cos(), angle.sin()
+    seq = torch.arange(B).int().cuda()
+    pos = torch.tensor([0, 777, 3000]).int().cuda()
+    lengths = pos + 1
+    size = nm.nmspmm_kv_attend_workspace_bytes(handle, heads * group, wide * page)
+    assert size > 0
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def step(out, turned, stream=None, workspace=ws):
+        nm.nmspmm_kv_append(handle, k, v, seq, pos, cos=cos, sin=sin, q=q, q_out=turned, stream=stream)
+        nm.nmspmm_kv_attend(handle, turned, lengths, out, stream=stream, workspace=workspace)
+
+    turned, first, out, bare_out = (torch.empty_like(q) for _ in range(4))
+    side = torch.cuda.Stream()
+    step(first, turned)
+    torch.cuda.synchronize()
+    step(out, turned, stream=side, workspace=None)
+    torch.cuda.synchronize()
+    assert torch.equal(out, first)
+    graph, bare = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, turned)
+    with torch.cuda.graph(bare):
+        step(bare_out, turned, workspace=None)
+    for _ in range(4):
+        pos += 5
+        lengths += 5
+        out.fill_(float("nan"))
+        bare_out.fill_(float("nan"))
+        graph.replay()
+        bare.replay()
+        torch.cuda.synchronize()
+        step(first, turned)
+        torch.cuda.synchronize()
+        assert torch.equal(out, first)
+        tol = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -14      # one split or several: the order of the sums
+        assert torch.all((bare_out.float() - first.float()).abs() <= tol * (first.float().abs() + 0.1))
