@@ -20,6 +20,8 @@ struct HalfEpilogue {
     int64_t ldc, ld_mul, ld_residual;
     float alpha;
     int act;
+    bool f32;               // C, mul and residual are fp32
+    bool vec;               // every row of every operand starts on 16 bytes
 };
 
 __device__ __forceinline__ float half_act(float y, int act)
@@ -39,6 +41,45 @@ __device__ __forceinline__ void half_store(const HalfEpilogue &e, int64_t i, int
     if (e.mul) y *= to_f32(static_cast<const O *>(e.mul)[i * e.ld_mul + j]);
     if (e.residual) y += to_f32(static_cast<const O *>(e.residual)[i * e.ld_residual + j]);
     static_cast<O *>(e.C)[i * e.ldc + j] = from_f32<O>(y);
+}
+
+// Eight columns of row i from column j on, all inside C.
+template <class O>
+__device__ __forceinline__ void half_store8(const HalfEpilogue &e, int64_t i, int64_t j, float (&y)[8])
+{
+    float z[8];
+    if (!e.vec) {
+#pragma unroll 1
+        for (int x = 0; x < 8; ++x) {
+            float v = y[0];     // (a dynamic index would put y into memory)
+#pragma unroll
+            for (int s = 1; s < 8; ++s) v = x == s ? y[s] : v;
+            half_store<O>(e, i, j + x, v);
+        }
+        return;
+    }
+#pragma unroll
+    for (int x = 0; x < 8; ++x) y[x] *= e.alpha;
+    if (e.bias) {
+        load_row<8, true>(e.bias + j, 8, z);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) y[x] += z[x];
+    }
+    if (e.act != NMSPMM_HALF_ACT_NONE) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) y[x] = half_act(y[x], e.act);
+    }
+    if (e.mul) {
+        load_row<8, true>(static_cast<const O *>(e.mul) + i * e.ld_mul + j, 8, z);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) y[x] *= z[x];
+    }
+    if (e.residual) {
+        load_row<8, true>(static_cast<const O *>(e.residual) + i * e.ld_residual + j, 8, z);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) y[x] += z[x];
+    }
+    store_row<8, true>(static_cast<O *>(e.C) + i * e.ldc + j, 8, y);
 }
 
 }  // namespace nmspmm

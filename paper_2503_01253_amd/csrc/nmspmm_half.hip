@@ -7,6 +7,8 @@
 #include <cstdio>
 
 #include "nmspmm_half.h"
+#include "nmspmm_half_tile.h"
+#include "nmspmm_half_tiles.h"
 #include "nmspmm_internal.h"
 #include "nmspmm_workspace.h"
 
@@ -17,20 +19,65 @@ bool aligned_to(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// The plain layout: Bc in 16 bits, then (256-byte aligned) idx.
-struct RawLayout {
-    int64_t w, q, idx_at, bytes;
+// ---- the packed weight -----------------------------------------------------
+//
+// Where V is a multiple of 16 the values lie as the matrix instruction reads
+// them (nmspmm_half_tile.h): MI columns by STEP compressed rows an operand, a
+// column tile's operands in the order of its units and steps; the offsets lie
+// in the same order, one per block and compressed row, as 16-bit columns of
+// the unit (PAD in padding rows), rows u and u + 4 of each eight side by side,
+// which is how a lane reads them.  Other widths keep Bc and idx as they are
+// (MI = 0).
+constexpr uint16_t PAD = 0xffff;
+
+struct HalfLayout {
+    int MI, STEP, G, S, KR;
+    int64_t w, q, windows, units, steps;    // units and steps of a column tile
+    int64_t offs_at, bytes;
 };
 
-RawLayout raw_layout(int64_t k, int64_t n, int N, int M, int V)
+HalfLayout half_layout(int64_t k, int64_t n, int N, int M, int V)
 {
-    RawLayout r;
-    r.w = k / M * N;
-    r.q = n / V;
-    r.idx_at = round_up(2 * r.w * n, 256);
-    r.bytes = r.idx_at + r.w * r.q;
-    return r;
+    HalfLayout l{};
+    l.windows = k / M;
+    l.w = l.windows * N;
+    l.q = n / V;
+    if (V % 16) {
+        l.offs_at = round_up(2 * l.w * n, 256);
+        l.bytes = l.offs_at + l.w * l.q;
+        return l;
+    }
+    l.MI = V % 32 ? 16 : 32;
+    l.STEP = 512 / l.MI;
+    // the fewest windows whose rows fill their operands best, within 128
+    // columns of A (which bound the LDS a stage takes)
+    double best = 0;
+    for (int G = 1; G == 1 || G * M <= 128; ++G) {
+        const int S = (G * N + l.STEP - 1) / l.STEP;
+        const double fill = (double)(G * N) / (S * l.STEP);
+        if (fill > best + 1e-9) {
+            best = fill;
+            l.G = G;
+            l.S = S;
+        }
+    }
+    l.KR = l.G * M;
+    l.units = (l.windows + l.G - 1) / l.G;
+    l.steps = l.units * l.S;
+    l.offs_at = round_up(n / l.MI * l.steps * 1024, 256);
+    l.bytes = l.offs_at + l.q * l.steps * 2 * l.STEP;
+    return l;
 }
+
+struct PackArgs {
+    const void *Bc;
+    const uint8_t *idx;
+    void *vals;
+    uint16_t *offs;
+    HalfLayout l;
+    int64_t n;
+    int N, M, V;
+};
 
 template <class T, class S>
 __global__ __launch_bounds__(256) void nm_half_pack_raw_kernel(const S *Bc, const uint8_t *idx, T *vals,
@@ -41,10 +88,54 @@ __global__ __launch_bounds__(256) void nm_half_pack_raw_kernel(const S *Bc, cons
     for (int64_t e = t; e < icount; e += stride) offs[e] = (uint8_t)(idx[e] < M ? idx[e] : M - 1);
 }
 
-struct RawArgs {
-    const void *A, *vals;
-    const uint8_t *offs;
-    int64_t lda, m, n, w, q;
+// The compressed row in place `slot` of unit `unit`, or -1 for padding.
+__device__ __forceinline__ int64_t packed_row(const PackArgs &p, int64_t unit, int slot, int &window_of_unit)
+{
+    window_of_unit = slot / p.N;
+    const int64_t window = unit * p.l.G + window_of_unit;
+    return slot < p.l.G * p.N && window < p.l.windows ? window * p.N + slot % p.N : -1;
+}
+
+template <class T, class S>
+__global__ __launch_bounds__(256) void nm_half_pack_kernel(PackArgs p)
+{
+    const int64_t stride = (int64_t)gridDim.x * 256, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int MI = p.l.MI, STEP = p.l.STEP;
+    const S *Bc = static_cast<const S *>(p.Bc);
+    T *vals = static_cast<T *>(p.vals);
+    const int64_t pieces = p.n / MI * p.l.steps * 64;       // of a lane's eight rows
+    for (int64_t e = t; e < pieces; e += stride) {
+        const int lane = (int)(e % 64);
+        const int64_t step = e / 64 % p.l.steps, tile = e / 64 / p.l.steps;
+        const int64_t col = tile * MI + lane % MI, unit = step / p.l.S;
+        const int first = (int)(step % p.l.S) * STEP + lane / MI * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            int win;
+            const int64_t u = packed_row(p, unit, first + j, win);
+            vals[e * 8 + j] = u < 0 ? from_f32<T>(0.f) : from_f32<T>(to_f32(Bc[u * p.n + col]));
+        }
+    }
+    const int64_t entries = p.l.q * p.l.steps * STEP;
+    for (int64_t e = t; e < entries; e += stride) {
+        const int at = (int)(e % STEP);
+        const int64_t step = e / STEP % p.l.steps, block = e / STEP / p.l.steps, unit = step / p.l.S;
+        const int slot = (int)(step % p.l.S) * STEP + at / 8 * 8 + at % 8 / 2 + 4 * (at % 2);
+        int win;
+        const int64_t u = packed_row(p, unit, slot, win);
+        const int o = u < 0 ? 0 : p.idx[u * p.l.q + block];
+        p.offs[e] = u < 0 ? PAD : (uint16_t)(win * p.M + (o < p.M ? o : p.M - 1));
+    }
+}
+
+// ---- any shape -------------------------------------------------------------
+
+struct GeneralArgs {
+    const void *A;
+    const void *vals;
+    const void *offs;
+    HalfLayout l;
+    int64_t lda, m, n;
     int N, M, V;
     HalfEpilogue epi;
 };
@@ -52,27 +143,41 @@ struct RawArgs {
 constexpr int HG_ROWS = 8;
 
 // Any shape: a thread owns one column and HG_ROWS rows of C and walks the
-// compressed rows; bound by the loads of A, one value per multiply-add.
+// compressed rows of either layout; bound by the loads of A, one value per
+// multiply-add .
 template <class T, class O>
-__global__ __launch_bounds__(256) void nm_half_general_kernel(RawArgs p)
+__global__ __launch_bounds__(256) void nm_half_general_kernel(GeneralArgs p)
 {
     const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (j >= p.n) return;
-    const T *A = static_cast<const T *>(p.A), *vals = static_cast<const T *>(p.vals) + j;
-    const uint8_t *offs = p.offs + j / p.V;
+    const T *A = static_cast<const T *>(p.A), *vals = static_cast<const T *>(p.vals);
     for (int64_t i0 = (int64_t)blockIdx.y * HG_ROWS; i0 < p.m; i0 += (int64_t)gridDim.y * HG_ROWS) {
         float sum[HG_ROWS] = {};
-        int64_t window = 0;
-        for (int64_t u = 0, r = 0; u < p.w; ++u) {
-            const float b = to_f32(vals[u * p.n]);
-            const T *a = A + i0 * p.lda + window + offs[u * p.q];
+        auto add = [&](int64_t at, float b) {
+            const T *a = A + i0 * p.lda + at;
 #pragma unroll
             for (int i = 0; i < HG_ROWS; ++i)
                 if (i0 + i < p.m) sum[i] = fmaf(to_f32(a[i * p.lda]), b, sum[i]);
-            if (++r == p.N) {
-                r = 0;
-                window += p.M;
+        };
+        if (p.l.MI == 0) {
+            const uint8_t *offs = static_cast<const uint8_t *>(p.offs) + j / p.V;
+            int64_t window = 0;
+            for (int64_t u = 0, r = 0; u < p.l.w; ++u) {
+                add(window + offs[u * p.l.q], to_f32(vals[u * p.n + j]));
+                if (++r == p.N) {
+                    r = 0;
+                    window += p.M;
+                }
             }
+        } else {
+            const uint16_t *offs = static_cast<const uint16_t *>(p.offs) + j / p.V * p.l.steps * p.l.STEP;
+            const T *tile = vals + (j / p.l.MI * p.l.steps * 64 + j % p.l.MI) * 8;
+            for (int64_t step = 0; step < p.l.steps; ++step)
+                for (int u = 0; u < p.l.STEP; ++u) {
+                    const uint16_t o = offs[step * p.l.STEP + u / 8 * 8 + u % 4 * 2 + u % 8 / 4];
+                    if (o != PAD)
+                        add(step / p.l.S * p.l.KR + o, to_f32(tile[(step * 64 + u / 8 * p.l.MI) * 8 + u % 8]));
+                }
         }
 #pragma unroll
         for (int i = 0; i < HG_ROWS; ++i)
@@ -81,13 +186,79 @@ __global__ __launch_bounds__(256) void nm_half_general_kernel(RawArgs p)
 }
 
 template <class T>
-hipError_t launch_general(const RawArgs &p, bool f32_out, hipStream_t stream)
+hipError_t launch_general(const GeneralArgs &p, hipStream_t stream)
 {
     const dim3 grid((unsigned)((p.n + 255) / 256),
                     (unsigned)std::min<int64_t>(65535, (p.m + HG_ROWS - 1) / HG_ROWS));
-    if (f32_out) hipLaunchKernelGGL((nm_half_general_kernel<T, float>), grid, dim3(256), 0, stream, p);
+    if (p.epi.f32) hipLaunchKernelGGL((nm_half_general_kernel<T, float>), grid, dim3(256), 0, stream, p);
     else hipLaunchKernelGGL((nm_half_general_kernel<T, T>), grid, dim3(256), 0, stream, p);
     return hipGetLastError();
+}
+
+// ---- the tiled kernel ------------------------------------------------------
+
+// The split parts of C added in order, then the epilogue.
+template <class O>
+__global__ __launch_bounds__(256) void nm_half_join_kernel(const float *part, int64_t m, int64_t n, int splits,
+                                                           HalfEpilogue epi)
+{
+    const int64_t stride = (int64_t)gridDim.x * 256;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < m * n; e += stride) {
+        float sum = 0.f;
+        for (int s = 0; s < splits; ++s) sum += part[s * m * n + e];
+        half_store<O>(epi, e / n, e % n, sum);
+    }
+}
+
+struct HalfPlan {
+    const HalfTileInfo *tile = nullptr;     // none: the general kernel
+    int P = 0, QS = 0, nst = 0, tiles_m = 0, tiles_n = 0, splits = 1;
+    int64_t ws_bytes = 0;
+};
+
+// An estimate of a tile's time, in cycles of a CU: rounds of tiles times the
+// larger of a tile's matrix work, its LDS traffic and what it loads from L2.
+double half_cost(const HalfTileInfo &t, const HalfLayout &l, int64_t tiles)
+{
+    const double rounds = (double)((tiles + 255) / 256);
+    const double slots = (double)l.units * l.S * l.STEP, cols = (double)l.units * l.KR;
+    const double mfma = 2.0 * t.BM * t.BN * slots / 4096;
+    const double lds = (slots * t.BM * 2 * (t.BN / (t.CT * t.MI)) + cols * t.BM * 2) / 100;
+    const double l2 = (cols * t.BM * 2 + slots * t.BN * 2) / 40;
+    return rounds * (std::max({mfma, lds, l2}) + 2000);
+}
+
+HalfPlan half_plan(int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w, bool may_split)
+{
+    HalfPlan best;
+    if (l.MI == 0 || w.k == 0 || w.k >= (int64_t)1 << 22) return best;
+    int count;
+    const HalfTileInfo *tiles = l.MI == 16 ? half_tiles_16(&count) : w.V % 64 ? half_tiles_32x1(&count)
+                                                                             : half_tiles_32x2(&count);
+    double best_cost = 1e300;
+    for (int i = 0; i < count; ++i) {
+        const HalfTileInfo &t = tiles[i];
+        const int unit_limit = t.kmax / l.KR;           // units a stage holds
+        int P = unit_limit / t.WK * t.WK;
+        if (P == 0) continue;
+        P = (int)std::min<int64_t>(P, round_up(l.units, t.WK));
+        const int64_t tiles_m = (m + t.BM - 1) / t.BM, tiles_n = (w.n + t.BN - 1) / t.BN;
+        if (tiles_m * tiles_n > ((int64_t)1 << 22)) continue;
+        HalfPlan c;
+        c.tile = &t;
+        c.P = P;
+        c.QS = P / t.WK * l.S;
+        c.nst = (int)((l.units + P - 1) / P);
+        c.tiles_m = (int)tiles_m;
+        c.tiles_n = (int)tiles_n;
+        const double cost = half_cost(t, l, tiles_m * tiles_n);
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = c;
+        }
+    }
+    (void)may_split;
+    return best;
 }
 
 nmspmm_status_t check_weight(const nmspmm_half_weight_t *w, int64_t m)
@@ -100,21 +271,98 @@ nmspmm_status_t check_weight(const nmspmm_half_weight_t *w, int64_t m)
 }
 
 template <class T>
-hipError_t pack_raw(const void *Bc, nmspmm_dtype_t type, const uint8_t *idx, const nmspmm_half_weight_t &w,
-                    hipStream_t stream)
+hipError_t pack(const void *Bc, nmspmm_dtype_t type, const uint8_t *idx, const nmspmm_half_weight_t &w,
+                hipStream_t stream)
 {
-    const RawLayout r = raw_layout(w.k, w.n, w.N, w.M, w.V);
-    T *vals = static_cast<T *>(const_cast<void *>(w.packed));
-    uint8_t *offs = static_cast<uint8_t *>(const_cast<void *>(w.packed)) + r.idx_at;
-    const int64_t count = r.w * w.n, icount = r.w * r.q;
+    PackArgs p{};
+    p.l = half_layout(w.k, w.n, w.N, w.M, w.V);
+    p.Bc = Bc;
+    p.idx = idx;
+    p.vals = const_cast<void *>(w.packed);
+    p.offs = reinterpret_cast<uint16_t *>(static_cast<char *>(p.vals) + p.l.offs_at);
+    p.n = w.n;
+    p.N = w.N;
+    p.M = w.M;
+    p.V = w.V;
+    const int64_t count = p.l.w * w.n, icount = p.l.w * p.l.q;
     const dim3 grid((unsigned)std::min<int64_t>(8192, (count + 255) / 256));
-    if (type == NMSPMM_F32)
-        hipLaunchKernelGGL((nm_half_pack_raw_kernel<T, float>), grid, dim3(256), 0, stream,
-                           static_cast<const float *>(Bc), idx, vals, offs, count, icount, w.M);
-    else
-        hipLaunchKernelGGL((nm_half_pack_raw_kernel<T, T>), grid, dim3(256), 0, stream, static_cast<const T *>(Bc),
-                           idx, vals, offs, count, icount, w.M);
+    if (p.l.MI == 0) {
+        T *vals = static_cast<T *>(p.vals);
+        uint8_t *offs = reinterpret_cast<uint8_t *>(p.offs);
+        if (type == NMSPMM_F32)
+            hipLaunchKernelGGL((nm_half_pack_raw_kernel<T, float>), grid, dim3(256), 0, stream,
+                               static_cast<const float *>(Bc), idx, vals, offs, count, icount, w.M);
+        else
+            hipLaunchKernelGGL((nm_half_pack_raw_kernel<T, T>), grid, dim3(256), 0, stream,
+                               static_cast<const T *>(Bc), idx, vals, offs, count, icount, w.M);
+    } else if (type == NMSPMM_F32) {
+        hipLaunchKernelGGL((nm_half_pack_kernel<T, float>), grid, dim3(256), 0, stream, p);
+    } else {
+        hipLaunchKernelGGL((nm_half_pack_kernel<T, T>), grid, dim3(256), 0, stream, p);
+    }
     return hipGetLastError();
+}
+
+template <class T>
+hipError_t run(const HalfPlan &c, const HalfLayout &l, const void *A, int64_t lda, const nmspmm_half_weight_t &w,
+               int64_t m, const HalfEpilogue &epi, void *workspace, hipStream_t stream)
+{
+    const char *base = static_cast<const char *>(w.packed);
+    if (!c.tile) {
+        GeneralArgs p{};
+        p.A = A;
+        p.vals = base;
+        p.offs = base + l.offs_at;
+        p.l = l;
+        p.lda = lda;
+        p.m = m;
+        p.n = w.n;
+        p.N = w.N;
+        p.M = w.M;
+        p.V = w.V;
+        p.epi = epi;
+        return launch_general<T>(p, stream);
+    }
+    HalfTileArgs p{};
+    p.A = A;
+    p.vals = reinterpret_cast<const unsigned char *>(base);
+    p.offs = reinterpret_cast<const uint16_t *>(base + l.offs_at);
+    p.part = static_cast<float *>(workspace);
+    p.lda = lda;
+    p.m = m;
+    p.n = w.n;
+    p.k = w.k;
+    p.V = w.V;
+    p.S = l.S;
+    p.KR = l.KR;
+    p.units = (int)l.units;
+    p.P = c.P;
+    p.QS = c.QS;
+    p.nst = c.nst;
+    p.tiles_m = c.tiles_m;
+    p.tiles_n = c.tiles_n;
+    p.splits = c.splits;
+    p.epi = epi;
+    // 16-byte loads of A: every row and every stage on 16 bytes
+    const bool vec = aligned_to(A, 16) && (m == 1 || lda % 8 == 0) && c.P * l.KR % 8 == 0;
+    hipError_t e = c.tile->launch(p, w.dtype == NMSPMM_BF16, vec, stream);
+    if (e == hipSuccess && c.splits > 1) {
+        const unsigned blocks = (unsigned)std::min<int64_t>(8192, (m * w.n + 255) / 256);
+        if (epi.f32)
+            hipLaunchKernelGGL((nm_half_join_kernel<float>), dim3(blocks), dim3(256), 0, stream, p.part, m, w.n, c.splits, epi);
+        else
+            hipLaunchKernelGGL((nm_half_join_kernel<T>), dim3(blocks), dim3(256), 0, stream, p.part, m, w.n, c.splits, epi);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+// The plan of a call: without a workspace, or where a row of A lies so far
+// from the next that a tile's rows span 2^31 bytes, other kernels run.
+HalfPlan plan_for(int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w, int64_t lda, bool may_split)
+{
+    if (lda >= (int64_t)1 << 22) return HalfPlan{};
+    return half_plan(m, l, w, may_split);
 }
 
 }  // namespace
@@ -126,7 +374,7 @@ extern "C" int64_t nmspmm_half_bytes(int64_t k, int64_t n, int N, int M, int V)
 {
     if (!shape_ok(0, n, k, N, M, V) || !sizes_fit(1, n, k)) return -1;
     if (k == 0 || n == 0) return 0;
-    return raw_layout(k, n, N, M, V).bytes;
+    return half_layout(k, n, N, M, V).bytes;
 }
 
 extern "C" nmspmm_status_t nmspmm_half_pack(const void *Bc, nmspmm_dtype_t bc_dtype, const uint8_t *idx,
@@ -138,21 +386,30 @@ extern "C" nmspmm_status_t nmspmm_half_pack(const void *Bc, nmspmm_dtype_t bc_dt
     if (weight->k == 0 || weight->n == 0) return NMSPMM_OK;
     if (!Bc || !idx || !weight->packed) return NMSPMM_ERR_INVALID_ARG;
     if (!aligned_to(Bc, dtype_bytes(bc_dtype)) || !aligned_to(weight->packed, 256)) return NMSPMM_ERR_UNSUPPORTED;
-    const hipError_t e = weight->dtype == NMSPMM_BF16 ? pack_raw<bf16_t>(Bc, bc_dtype, idx, *weight, stream)
-                                                      : pack_raw<f16_t>(Bc, bc_dtype, idx, *weight, stream);
+    const hipError_t e = weight->dtype == NMSPMM_BF16 ? pack<bf16_t>(Bc, bc_dtype, idx, *weight, stream)
+                                                      : pack<f16_t>(Bc, bc_dtype, idx, *weight, stream);
     return e == hipSuccess ? NMSPMM_OK : NMSPMM_ERR_HIP;
 }
 
 extern "C" int64_t nmspmm_half_workspace_bytes(int64_t m, const nmspmm_half_weight_t *weight)
 {
-    return check_weight(weight, m) == NMSPMM_OK ? 0 : -1;
+    if (check_weight(weight, m) != NMSPMM_OK) return -1;
+    if (m == 0 || weight->n == 0) return 0;
+    const HalfLayout l = half_layout(weight->k, weight->n, weight->N, weight->M, weight->V);
+    return half_plan(m, l, *weight, true).ws_bytes;
 }
 
-extern "C" const char *nmspmm_half_kernel_name(int64_t m, const nmspmm_half_weight_t *weight, int)
+extern "C" const char *nmspmm_half_kernel_name(int64_t m, const nmspmm_half_weight_t *weight, int with_workspace)
 {
     if (check_weight(weight, m) != NMSPMM_OK) return "invalid";
     if (m == 0 || weight->n == 0) return "none";
-    return "nm_half_general_kernel";
+    const HalfLayout l = half_layout(weight->k, weight->n, weight->N, weight->M, weight->V);
+    const HalfPlan c = half_plan(m, l, *weight, with_workspace != 0);
+    if (!c.tile) return "nm_half_general_kernel";
+    thread_local char buf[128];
+    std::snprintf(buf, sizeof buf, "nm_half_tile_kernel<%dx%d,mi%d,wk%d>,stage%d,split%d", c.tile->BM, c.tile->BN,
+                  c.tile->MI, c.tile->WK, c.P * l.KR, c.splits);
+    return buf;
 }
 
 extern "C" nmspmm_status_t nmspmm_half_run(const void *A, int64_t lda, const nmspmm_half_weight_t *weight, void *C,
@@ -175,21 +432,20 @@ extern "C" nmspmm_status_t nmspmm_half_run(const void *A, int64_t lda, const nms
         !aligned_to(mul, cs) || !aligned_to(residual, cs) || !aligned_to(workspace, 256))
         return NMSPMM_ERR_UNSUPPORTED;
     if (!sizes_fit(m, std::max({ldc, ld_mul, ld_residual}), lda)) return NMSPMM_ERR_UNSUPPORTED;
-    const RawLayout r = raw_layout(w.k, w.n, w.N, w.M, w.V);
-    RawArgs p{};
-    p.A = A;
-    p.vals = w.packed;
-    p.offs = static_cast<const uint8_t *>(w.packed) + r.idx_at;
-    p.lda = lda;
-    p.m = m;
-    p.n = w.n;
-    p.w = r.w;
-    p.q = r.q;
-    p.N = w.N;
-    p.M = w.M;
-    p.V = w.V;
-    p.epi = {C, bias, mul, residual, ldc, ld_mul, ld_residual, alpha, act};
-    const hipError_t e = w.dtype == NMSPMM_BF16 ? launch_general<bf16_t>(p, c_dtype == NMSPMM_F32, stream)
-                                                : launch_general<f16_t>(p, c_dtype == NMSPMM_F32, stream);
-    return e == hipSuccess ? NMSPMM_OK : NMSPMM_ERR_HIP;
+    const HalfLayout l = half_layout(w.k, w.n, w.N, w.M, w.V);
+    if (m == 1) lda = w.k;
+    const auto rows16 = [cs](const void *ptr, int64_t ld) { return !ptr || (aligned_to(ptr, 16) && ld * cs % 16 == 0); };
+    const HalfEpilogue epi = {C, bias, mul, residual, ldc, ld_mul, ld_residual, alpha, act, c_dtype == NMSPMM_F32,
+                              rows16(C, ldc) && rows16(mul, ld_mul) && rows16(residual, ld_residual) &&
+                                  aligned_to(bias, 16)};
+    int cached = -1;
+    HalfPlan c = plan_for(m, l, w, lda, true);
+    if (c.ws_bytes > 0 && (!workspace || (uint64_t)c.ws_bytes > (uint64_t)workspace_bytes)) {
+        workspace = capturing(stream) ? nullptr : ws_acquire(stream, (size_t)c.ws_bytes, &cached);
+        if (!workspace) c = plan_for(m, l, w, lda, false);
+    }
+    const hipError_t e = w.dtype == NMSPMM_BF16 ? run<bf16_t>(c, l, A, lda, w, m, epi, workspace, stream)
+                                                : run<f16_t>(c, l, A, lda, w, m, epi, workspace, stream);
+    const hipError_t f = cached >= 0 ? ws_done(cached, stream) : hipSuccess;
+    return e == hipSuccess && f == hipSuccess ? NMSPMM_OK : NMSPMM_ERR_HIP;
 }

@@ -1,0 +1,376 @@
+// Tiled kernel of the 16-bit N:M product (device code, included by the units
+// that instantiate it).
+//
+// The packed weight (nmspmm_half_pack) holds the matrix instruction's B
+// operands as its lanes read them.  MI columns (32 where V is a multiple of
+// 32, else 16) and STEP = 512/MI compressed rows make one operand: 64 lanes of
+// eight consecutive rows, 1 KB in one piece.  Compressed rows are counted in
+// units of G whole windows (KR = G*M columns of A, G*N rows padded to S
+// operands), and every padding row has an offset of its own kind.
+//
+// A workgroup of WR x WC x WK waves owns BM x BN outputs (and, with split-k,
+// one slice of k).  It walks k in stages of P units:
+//   A_s : the BM x P*KR slab of A in LDS, k-major: row c holds column c of A,
+//         BM rows of C, 16 to a granule of 32 bytes; one last row of zeros is
+//         where padding offsets lead, so that no value of A meets a padding
+//         row's zero.  Global -> registers (4 rows x 8 columns a block) ->
+//         transposed by byte permutes -> LDS, one stage ahead, two slots.
+//   gather: ds_read_b64_tr_b16 hands 16 lanes four LDS rows of 16 outputs,
+//         each row at its own address, already transposed into the A operand:
+//         the gather of Eq. 1 costs nothing beyond the read.
+//   B, offsets: straight from memory into registers, two operands ahead.
+// Granule g of row c lies at place g ^ swz(c), which spreads a transposed read
+// over the banks.  The WK waves of a tile share out the units of every stage
+// and are joined through LDS at the end.
+#ifndef NMSPMM_HALF_TILE_H
+#define NMSPMM_HALF_TILE_H
+
+#include "nmspmm_half.h"
+#include "nmspmm_tiled.h"
+
+namespace nmspmm {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+
+struct HalfTileArgs {
+    const void *A;
+    const unsigned char *vals;
+    const uint16_t *offs;
+    float *part;            // with split-k: splits x m x n partial sums
+    int64_t lda, m, n, k;
+    int32_t V, S, KR, units, P, QS, nst;
+    int32_t tiles_m, tiles_n, splits;
+    HalfEpilogue epi;
+};
+
+template <int MI> struct MfmaAcc;
+template <> struct MfmaAcc<32> { typedef f32x16 type; static constexpr int E = 16; };
+template <> struct MfmaAcc<16> { typedef f32x4 type; static constexpr int E = 4; };
+
+template <class T, int MI>
+__device__ __forceinline__ typename MfmaAcc<MI>::type half_mfma(s16x8 a, s16x8 b, typename MfmaAcc<MI>::type c)
+{
+    if constexpr (__is_same(T, bf16_t)) {
+        const bf16x8 x = __builtin_bit_cast(bf16x8, a), y = __builtin_bit_cast(bf16x8, b);
+        if constexpr (MI == 32) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+    } else {
+        const f16x8 x = __builtin_bit_cast(f16x8, a), y = __builtin_bit_cast(f16x8, b);
+        if constexpr (MI == 32) return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, c, 0, 0, 0);
+        else return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
+    }
+}
+
+// The shape of a tile: MI x MI accumulators, RT of them down a wave's rows and
+// CT across the columns of each of its NG gathers; NB blocks of A a thread
+// and stage; LDS_KB of LDS.
+template <int MI_, int CT_, int NG_, int RT_, int WR_, int WC_, int WK_, int NB_, int LDS_KB_>
+struct HalfTile {
+    static constexpr int MI = MI_, CT = CT_, NG = NG_, RT = RT_, WR = WR_, WC = WC_, WK = WK_, NB = NB_;
+    static constexpr int BM = MI * RT * WR, BN = MI * CT * NG * WC, NT = 64 * WR * WC * WK;
+    static constexpr int STEP = 512 / MI, PITCH = 2 * BM, LDS_BYTES = 1024 * LDS_KB_;
+    static constexpr int ACCS = RT * CT * NG;
+    // waves a SIMD: two workgroups a CU where their LDS leaves room
+    static constexpr int WPS = NT / 256 * (LDS_KB_ <= 80 ? 2 : 1);
+    static constexpr int RED_BYTES = WK > 1 ? (WK / 2) * WR * WC * ACCS * MI * MI * 4 : 0;
+    static constexpr int CW = CT * NG * MI, CPITCH = CW + 4;        // a wave's columns
+    static_assert((RT & (RT - 1)) == 0 && RED_BYTES <= LDS_BYTES && WR * WC * WK * MI * CPITCH * 4 <= LDS_BYTES &&
+                      64 / (CW / 8) <= MI, "tile shape");
+    // columns of A of a stage at most: by LDS (two slots with their row of zeros) and by registers
+    static constexpr int KMAX_LDS = (LDS_BYTES / 2 / PITCH - 1) / 8 * 8;
+    static constexpr int KMAX_REG = NB * NT / BM * 4 * 8;
+    static constexpr int KMAX = KMAX_LDS < KMAX_REG ? KMAX_LDS : KMAX_REG;
+    // place of LDS row c's granules: consecutive rows on different banks
+    __device__ static constexpr int swz(int c)
+    {
+        if (MI == 32) return BM >= 128 ? (c & 3) << 1 : BM == 64 ? c & 2 : 0;
+        return BM >= 128 ? c & 7 : BM == 64 ? (c >> 1) & 3 : BM == 32 ? (c >> 2) & 1 : 0;
+    }
+};
+
+// Rows 4 x columns 8 of 16-bit values, transposed: out[j] holds column j.
+__device__ __forceinline__ void transpose_4x8(const u32x4 (&r)[4], u32x2 (&out)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        out[2 * j] = u32x2{__builtin_amdgcn_perm(r[1][j], r[0][j], 0x05040100u),
+                           __builtin_amdgcn_perm(r[3][j], r[2][j], 0x05040100u)};
+        out[2 * j + 1] = u32x2{__builtin_amdgcn_perm(r[1][j], r[0][j], 0x07060302u),
+                               __builtin_amdgcn_perm(r[3][j], r[2][j], 0x07060302u)};
+    }
+}
+
+template <class T, class C, bool VEC>
+__global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArgs p)
+{
+    constexpr int MI = C::MI, CT = C::CT, NG = C::NG, RT = C::RT, WR = C::WR, WC = C::WC, WK = C::WK, NB = C::NB;
+    constexpr int BM = C::BM, BN = C::BN, NT = C::NT, STEP = C::STEP, PITCH = C::PITCH;
+    typedef typename MfmaAcc<MI>::type acc_t;
+    constexpr int E = MfmaAcc<MI>::E;
+    __shared__ __align__(256) unsigned char lds[C::LDS_BYTES];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wk = wave / (WR * WC), wr = wave / WC % WR, wc = wave % WC;
+    int tm, tn, split;
+    map_tile(blockIdx.x, gridDim.x, p.tiles_m, p.tiles_n, tm, tn, split);
+    const int64_t row0 = (int64_t)tm * BM, col0 = (int64_t)tn * BN;
+    const int sps = (p.nst + p.splits - 1) / p.splits;
+    const int s_begin = split * sps, s_end = min(p.nst, s_begin + sps);
+
+    // ---- A: global -> registers -> LDS ----
+    const int kstage = p.P * p.KR, chunks = (kstage + 7) / 8, zero_row = chunks * 8;
+    const int slot_bytes = (zero_row + 1) * PITCH;
+    const int rows_valid = (int)min64(BM, p.m - row0);
+    const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(static_cast<const T *>(p.A) + row0 * p.lda,
+                                                    (uint32_t)(((rows_valid - 1) * p.lda + p.k) * 2));
+    u32x4 ra[NB][4];
+    // block b of this thread: rows 4*rb.., columns 8*kc.. of the stage
+    auto block_rb = [&](int b) { return ((tid + b * NT) >> 2) % (BM / 4); };
+    auto block_kc = [&](int b) { return (tid & 3) + 4 * ((tid + b * NT) / BM); };
+    auto load_a = [&](int st) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int rb = block_rb(b), kc = block_kc(b);
+            const int64_t kpos = (int64_t)st * kstage + 8 * kc;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool ok = kc < chunks && 4 * rb + r < rows_valid && kpos < p.k;
+                const uint32_t off = (uint32_t)(((4 * rb + r) * p.lda + kpos) * 2);
+                if constexpr (VEC) {
+                    ra[b][r] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, (int)(ok ? off : OOB), 0, 0));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(ok ? off + 4 * j : OOB), 0, 0);
+                        const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(ok ? off + 4 * j + 2 : OOB), 0, 0);
+                        ra[b][r][j] = (lo & 0xffffu) | hi << 16;
+                    }
+                }
+            }
+        }
+    };
+    auto store_a = [&](int slot) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int rb = block_rb(b), kc = block_kc(b);
+            if (kc < chunks) {
+                u32x2 col[8];
+                transpose_4x8(ra[b], col);
+                unsigned char *dst = lds + slot * slot_bytes + kc * 8 * PITCH;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<u32x2 *>(dst + j * PITCH + (((rb >> 2) ^ C::swz(j)) << 5) + 8 * (rb & 3)) = col[j];
+            }
+        }
+    };
+
+    // ---- B operands and offsets, two steps ahead ----
+    const int nsteps = p.units * p.S;
+    const uint32_t ctiles = (uint32_t)(p.n / MI);
+    const unsigned char *bp[NG][CT];
+    const unsigned char *op[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        const uint32_t first = (uint32_t)(col0 / MI) + (wc * NG + g) * CT;
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+            bp[g][c] = p.vals + (int64_t)min(first + c, ctiles - 1) * nsteps * 1024;
+        op[g] = reinterpret_cast<const unsigned char *>(p.offs) + (int64_t)(min(first, ctiles - 1) * MI / p.V) * nsteps * (2 * STEP);
+    }
+    const int pair = (lane / MI) * 4 + ((lane >> 2) & 3);
+    s16x8 rb_[2][NG][CT];
+    uint32_t ro[2][NG];
+    // a wave's steps in order: QS consecutive ones of every stage
+    struct Cursor {
+        int q, s, rows, step;
+    };
+    const int PW = p.P / WK;
+    auto advance = [&](Cursor &c) {
+        ++c.step;
+        if (++c.s == p.S) {
+            c.s = 0;
+            c.rows += p.KR;
+        }
+        if (++c.q == p.QS) {
+            c.q = 0;
+            c.rows = wk * PW * p.KR;
+            c.step += p.P * p.S - p.QS;
+        }
+    };
+    auto load_b = [&](int i, const Cursor &c) {
+        const int step = min(c.step, nsteps - 1);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+                rb_[i][g][t] = *reinterpret_cast<const s16x8 *>(bp[g][t] + (int64_t)step * 1024 + lane * 16);
+            ro[i][g] = *reinterpret_cast<const uint32_t *>(op[g] + (int64_t)step * (2 * STEP) + pair * 4);
+        }
+    };
+
+    acc_t acc[NG][RT][CT];
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[g][t][c][e] = 0.f;
+
+    // where a lane of a transposed read looks: its piece of 4 outputs, and (MI
+    // = 32) its granule of the pair
+    const int piece = 8 * (lane & 3) + (MI == 32 ? 32 * ((lane >> 4) & 1) : 0);
+    constexpr int TSHIFT = MI == 32 ? 6 : 5;
+    const int g0 = wr * RT << TSHIFT;
+
+    auto compute = [&](int i, const Cursor &c, uint32_t slot) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            uint32_t at[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t off = x == 0 ? ro[i][g] & 0xffffu : ro[i][g] >> 16;
+                const uint32_t row = min(off + (uint32_t)c.rows, (uint32_t)zero_row);
+                at[x] = slot + row * PITCH + (g0 ^ (C::swz(row) << 5)) + piece;
+            }
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                s16x4 v[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    v[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(lds_u8 *)(uintptr_t)(at[x] ^ (t << TSHIFT)));
+                const s16x8 a = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) acc[g][t][ct] = half_mfma<T, MI>(a, rb_[i][g][ct], acc[g][t][ct]);
+            }
+        }
+    };
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8 *)(lds_void *)lds;
+    if (s_begin < s_end) {
+        // the rows of zeros of both slots
+        for (int i = tid; i < 2 * (PITCH / 4); i += NT)
+            *reinterpret_cast<uint32_t *>(lds + i / (PITCH / 4) * slot_bytes + zero_row * PITCH + i % (PITCH / 4) * 4) = 0;
+        load_a(s_begin);
+        Cursor use{0, 0, wk * PW * p.KR, (s_begin * p.P + wk * PW) * p.S}, ahead = use;
+        load_b(0, ahead);
+        advance(ahead);
+        load_b(1, ahead);
+        advance(ahead);
+        store_a(0);
+        lds_sync();
+        if (s_begin + 1 < s_end) load_a(s_begin + 1);
+        int st = s_begin, slot = 0;
+        auto step = [&](int i) {
+            if (use.step < nsteps) compute(i, use, lds0 + slot * slot_bytes);
+            load_b(i, ahead);
+            advance(ahead);
+            advance(use);
+            if (use.q == 0) {
+                ++st;
+                slot ^= 1;
+                if (st < s_end) {
+                    store_a(slot);
+                    lds_sync();
+                    if (st + 1 < s_end) load_a(st + 1);
+                }
+            }
+        };
+        while (true) {
+            step(0);
+            if (st >= s_end) break;
+            step(1);
+            if (st >= s_end) break;
+        }
+    }
+
+    // ---- the WK waves of a tile, joined in a fixed order ----
+    if constexpr (WK > 1) {
+        float *red = reinterpret_cast<float *>(lds);
+        const int pos = wr * WC + wc;
+#pragma unroll
+        for (int half = WK / 2; half >= 1; half /= 2) {
+            lds_sync();
+            float *mine = red + (((wk >= half ? wk - half : wk) * WR * WC + pos) * C::ACCS * E) * 64 + lane;
+            if (wk >= half && wk < 2 * half) {
+                int i = 0;
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t)
+#pragma unroll
+                        for (int c = 0; c < CT; ++c)
+#pragma unroll
+                            for (int e = 0; e < E; ++e) mine[64 * i++] = acc[g][t][c][e];
+            }
+            lds_sync();
+            if (wk < half) {
+                int i = 0;
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t)
+#pragma unroll
+                        for (int c = 0; c < CT; ++c)
+#pragma unroll
+                            for (int e = 0; e < E; ++e) acc[g][t][c][e] += mine[64 * i++];
+            }
+        }
+    }
+
+    // ---- C: every wave turns its accumulators, MI rows at a time, in a piece
+    // of LDS of its own, so that a lane stores eight columns of one row.
+    // Element e of lane l: row 8*(e/4) + 4*(l/32) + e%4 (MI = 32) or
+    // 4*(l/16) + e of the accumulator, column l % MI ----
+    lds_sync();
+    if (wk > 0) return;
+    constexpr int CW = C::CW, CP = C::CPITCH, LPR = CW / 8, RPP = 64 / LPR;
+    float *turn = reinterpret_cast<float *>(lds) + wave * (MI * CP);
+    const int64_t j = col0 + wc * CW + lane % LPR * 8;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int r = MI == 32 ? 8 * (e / 4) + 4 * (lane / 32) + e % 4 : 4 * (lane / 16) + e;
+                    turn[r * CP + (g * CT + c) * MI + lane % MI] = acc[g][t][c][e];
+                }
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int r = 0; r < MI; r += RPP) {
+            const int row = r + lane / LPR;
+            const int64_t i = row0 + (wr * RT + t) * MI + row;
+            float x[8];
+            const f32x4 lo = *reinterpret_cast<const f32x4 *>(turn + row * CP + lane % LPR * 8);
+            const f32x4 hi = *reinterpret_cast<const f32x4 *>(turn + row * CP + lane % LPR * 8 + 4);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                x[y] = lo[y];
+                x[4 + y] = hi[y];
+            }
+            if (row < MI && i < p.m && j < p.n) {
+                if (p.splits > 1) store_row<8, true>(p.part + ((int64_t)split * p.m + i) * p.n + j, 8, x);
+                else if (p.epi.f32) half_store8<float>(p.epi, i, j, x);
+                else half_store8<T>(p.epi, i, j, x);
+            }
+        }
+        asm volatile("" ::: "memory");
+    }
+}
+
+}  // namespace nmspmm
+
+#endif

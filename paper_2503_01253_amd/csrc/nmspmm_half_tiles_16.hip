@@ -1,0 +1,19 @@
+// The tiled kernel's instantiations for 16-column gathers.
+#include "nmspmm_half_launch.h"
+
+namespace nmspmm {
+
+const HalfTileInfo *half_tiles_16(int *count)
+{
+    //                          MI CT NG RT WR WC WK NB LDS
+    static const HalfTileInfo list[] = {
+        half_tile_info<HalfTile<16, 1, 2, 16, 1, 8, 1, 2, 160>>(),
+        half_tile_info<HalfTile<16, 1, 2, 8, 1, 4, 2, 1, 80>>(),
+        half_tile_info<HalfTile<16, 1, 2, 4, 1, 2, 4, 1, 80>>(),
+        half_tile_info<HalfTile<16, 1, 2, 2, 1, 1, 8, 1, 80>>(),
+    };
+    *count = sizeof list / sizeof list[0];
+    return list;
+}
+
+}  // namespace nmspmm
