@@ -26,8 +26,9 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // column tile's operands in the order of its units and steps; the offsets lie
 // in the same order, one per block and compressed row, as 16-bit columns of
 // the unit (PAD in padding rows), rows u and u + 4 of each eight side by side,
-// which is how a lane reads them.  Other widths keep Bc and idx as they are
-// (MI = 0).
+// which is how a lane reads them, and a block's end with a step of padding.
+// Other widths, and windows of so many kept rows that no stage holds them,
+// keep Bc and idx as they are (MI = 0).
 constexpr uint16_t PAD = 0xffff;
 
 struct HalfLayout {
@@ -42,7 +43,7 @@ HalfLayout half_layout(int64_t k, int64_t n, int N, int M, int V)
     l.windows = k / M;
     l.w = l.windows * N;
     l.q = n / V;
-    if (V % 16) {
+    if (V % 16 || N > HALF_MAX_QS * (V % 32 ? 32 : 16)) {
         l.offs_at = round_up(2 * l.w * n, 256);
         l.bytes = l.offs_at + l.w * l.q;
         return l;
@@ -50,10 +51,12 @@ HalfLayout half_layout(int64_t k, int64_t n, int N, int M, int V)
     l.MI = V % 32 ? 16 : 32;
     l.STEP = 512 / l.MI;
     // the fewest windows whose rows fill their operands best, within 128
-    // columns of A (which bound the LDS a stage takes)
+    // columns of A (which bound the LDS a stage takes) and the operands of a
+    // stage
     double best = 0;
     for (int G = 1; G == 1 || G * M <= 128; ++G) {
         const int S = (G * N + l.STEP - 1) / l.STEP;
+        if (S > HALF_MAX_QS) break;
         const double fill = (double)(G * N) / (S * l.STEP);
         if (fill > best + 1e-9) {
             best = fill;
@@ -65,7 +68,7 @@ HalfLayout half_layout(int64_t k, int64_t n, int N, int M, int V)
     l.units = (l.windows + l.G - 1) / l.G;
     l.steps = l.units * l.S;
     l.offs_at = round_up(n / l.MI * l.steps * 1024, 256);
-    l.bytes = l.offs_at + l.q * l.steps * 2 * l.STEP;
+    l.bytes = l.offs_at + l.q * (l.steps + 1) * 2 * l.STEP;
     return l;
 }
 
@@ -116,10 +119,10 @@ __global__ __launch_bounds__(256) void nm_half_pack_kernel(PackArgs p)
             vals[e * 8 + j] = u < 0 ? from_f32<T>(0.f) : from_f32<T>(to_f32(Bc[u * p.n + col]));
         }
     }
-    const int64_t entries = p.l.q * p.l.steps * STEP;
+    const int64_t entries = p.l.q * (p.l.steps + 1) * STEP;
     for (int64_t e = t; e < entries; e += stride) {
         const int at = (int)(e % STEP);
-        const int64_t step = e / STEP % p.l.steps, block = e / STEP / p.l.steps, unit = step / p.l.S;
+        const int64_t step = e / STEP % (p.l.steps + 1), block = e / STEP / (p.l.steps + 1), unit = step / p.l.S;
         const int slot = (int)(step % p.l.S) * STEP + at / 8 * 8 + at % 8 / 2 + 4 * (at % 2);
         int win;
         const int64_t u = packed_row(p, unit, slot, win);
@@ -170,7 +173,7 @@ __global__ __launch_bounds__(256) void nm_half_general_kernel(GeneralArgs p)
                 }
             }
         } else {
-            const uint16_t *offs = static_cast<const uint16_t *>(p.offs) + j / p.V * p.l.steps * p.l.STEP;
+            const uint16_t *offs = static_cast<const uint16_t *>(p.offs) + j / p.V * (p.l.steps + 1) * p.l.STEP;
             const T *tile = vals + (j / p.l.MI * p.l.steps * 64 + j % p.l.MI) * 8;
             for (int64_t step = 0; step < p.l.steps; ++step)
                 for (int u = 0; u < p.l.STEP; ++u) {
@@ -210,9 +213,23 @@ __global__ __launch_bounds__(256) void nm_half_join_kernel(const float *part, in
     }
 }
 
+struct HalfTileInfo {
+    int MI, CT, WK, BM, BN, NT, kmax, per_cu;
+    bool any;       // takes any alignment of A
+};
+
+#define NMSPMM_HALF_INFO(MI, CT, NG, RT, WR, WC, WK, NB, LDS, ANY)                                               \
+    {MI, CT, WK, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::BM, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::BN, \
+     HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::NT, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::KMAX, 160 / LDS, \
+     ANY != 0},
+const HalfTileInfo half_tiles[] = {NMSPMM_HALF_TILES(NMSPMM_HALF_INFO)};
+#undef NMSPMM_HALF_INFO
+constexpr int half_tile_count = sizeof half_tiles / sizeof half_tiles[0];
+
 struct HalfPlan {
-    const HalfTileInfo *tile = nullptr;     // none: the general kernel
-    int P = 0, QS = 0, nst = 0, tiles_m = 0, tiles_n = 0, splits = 1;
+    int tile = -1;      // none: the general kernel
+    int QS = 0, P = 0, nst = 0, tiles_m = 0, tiles_n = 0, splits = 1;
+    bool vec = true;
     int64_t ws_bytes = 0;
 };
 
@@ -228,27 +245,28 @@ double half_cost(const HalfTileInfo &t, const HalfLayout &l, int64_t tiles)
     return rounds * (std::max({mfma, lds, l2}) + 2000);
 }
 
-HalfPlan half_plan(int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w, bool may_split)
+// vec: A's rows start on 16 bytes.
+HalfPlan half_plan(int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w, bool vec, bool may_split)
 {
     HalfPlan best;
     if (l.MI == 0 || w.k == 0 || w.k >= (int64_t)1 << 22) return best;
-    int count;
-    const HalfTileInfo *tiles = l.MI == 16 ? half_tiles_16(&count) : w.V % 64 ? half_tiles_32x1(&count)
-                                                                             : half_tiles_32x2(&count);
     double best_cost = 1e300;
-    for (int i = 0; i < count; ++i) {
-        const HalfTileInfo &t = tiles[i];
-        const int unit_limit = t.kmax / l.KR;           // units a stage holds
-        int P = unit_limit / t.WK * t.WK;
-        if (P == 0) continue;
-        P = (int)std::min<int64_t>(P, round_up(l.units, t.WK));
+    for (int i = 0; i < half_tile_count; ++i) {
+        const HalfTileInfo &t = half_tiles[i];
+        if (t.MI != l.MI) continue;
+        HalfPlan c;
+        c.tile = i;
+        // the longest stage that LDS and registers hold
+        for (int QS = HALF_MAX_QS; QS >= 1 && c.QS == 0; --QS)
+            if (QS % l.S == 0 && QS / l.S * t.WK * l.KR <= t.kmax) c.QS = QS;
+        if (c.QS == 0) continue;
+        c.P = c.QS / l.S * t.WK;
+        c.vec = vec && c.P * l.KR % 8 == 0;
+        if (!c.vec && !t.any) continue;
+        if (w.V % (t.CT * t.MI)) continue;
         const int64_t tiles_m = (m + t.BM - 1) / t.BM, tiles_n = (w.n + t.BN - 1) / t.BN;
         if (tiles_m * tiles_n > ((int64_t)1 << 22)) continue;
-        HalfPlan c;
-        c.tile = &t;
-        c.P = P;
-        c.QS = P / t.WK * l.S;
-        c.nst = (int)((l.units + P - 1) / P);
+        c.nst = (int)((l.units + c.P - 1) / c.P);
         c.tiles_m = (int)tiles_m;
         c.tiles_n = (int)tiles_n;
         const double cost = half_cost(t, l, tiles_m * tiles_n);
@@ -308,7 +326,7 @@ hipError_t run(const HalfPlan &c, const HalfLayout &l, const void *A, int64_t ld
                int64_t m, const HalfEpilogue &epi, void *workspace, hipStream_t stream)
 {
     const char *base = static_cast<const char *>(w.packed);
-    if (!c.tile) {
+    if (c.tile < 0) {
         GeneralArgs p{};
         p.A = A;
         p.vals = base;
@@ -335,17 +353,18 @@ hipError_t run(const HalfPlan &c, const HalfLayout &l, const void *A, int64_t ld
     p.V = w.V;
     p.S = l.S;
     p.KR = l.KR;
-    p.units = (int)l.units;
     p.P = c.P;
-    p.QS = c.QS;
+    p.steps = (int)l.steps;
     p.nst = c.nst;
     p.tiles_m = c.tiles_m;
     p.tiles_n = c.tiles_n;
     p.splits = c.splits;
     p.epi = epi;
-    // 16-byte loads of A: every row and every stage on 16 bytes
-    const bool vec = aligned_to(A, 16) && (m == 1 || lda % 8 == 0) && c.P * l.KR % 8 == 0;
-    hipError_t e = c.tile->launch(p, w.dtype == NMSPMM_BF16, vec, stream);
+    const bool bf16 = w.dtype == NMSPMM_BF16;
+    hipError_t e = c.QS == 1 ? launch_half_q1(c.tile, p, bf16, c.vec, stream)
+                 : c.QS == 2 ? launch_half_q2(c.tile, p, bf16, c.vec, stream)
+                 : c.QS == 3 ? launch_half_q3(c.tile, p, bf16, c.vec, stream)
+                             : launch_half_q4(c.tile, p, bf16, c.vec, stream);
     if (e == hipSuccess && c.splits > 1) {
         const unsigned blocks = (unsigned)std::min<int64_t>(8192, (m * w.n + 255) / 256);
         if (epi.f32)
@@ -357,12 +376,13 @@ hipError_t run(const HalfPlan &c, const HalfLayout &l, const void *A, int64_t ld
     return e;
 }
 
-// The plan of a call: without a workspace, or where a row of A lies so far
-// from the next that a tile's rows span 2^31 bytes, other kernels run.
-HalfPlan plan_for(int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w, int64_t lda, bool may_split)
+// The plan of a call.  Where a row of A lies so far from the next that a
+// tile's rows span 2^31 bytes, the general kernel runs.
+HalfPlan plan_for(const void *A, int64_t lda, int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w,
+                  bool may_split)
 {
     if (lda >= (int64_t)1 << 22) return HalfPlan{};
-    return half_plan(m, l, w, may_split);
+    return half_plan(m, l, w, aligned_to(A, 16) && (m == 1 || lda % 8 == 0), may_split);
 }
 
 }  // namespace
@@ -396,7 +416,7 @@ extern "C" int64_t nmspmm_half_workspace_bytes(int64_t m, const nmspmm_half_weig
     if (check_weight(weight, m) != NMSPMM_OK) return -1;
     if (m == 0 || weight->n == 0) return 0;
     const HalfLayout l = half_layout(weight->k, weight->n, weight->N, weight->M, weight->V);
-    return half_plan(m, l, *weight, true).ws_bytes;
+    return half_plan(m, l, *weight, true, true).ws_bytes;
 }
 
 extern "C" const char *nmspmm_half_kernel_name(int64_t m, const nmspmm_half_weight_t *weight, int with_workspace)
@@ -404,11 +424,12 @@ extern "C" const char *nmspmm_half_kernel_name(int64_t m, const nmspmm_half_weig
     if (check_weight(weight, m) != NMSPMM_OK) return "invalid";
     if (m == 0 || weight->n == 0) return "none";
     const HalfLayout l = half_layout(weight->k, weight->n, weight->N, weight->M, weight->V);
-    const HalfPlan c = half_plan(m, l, *weight, with_workspace != 0);
-    if (!c.tile) return "nm_half_general_kernel";
+    const HalfPlan c = half_plan(m, l, *weight, true, with_workspace != 0);
+    if (c.tile < 0) return "nm_half_general_kernel";
     thread_local char buf[128];
-    std::snprintf(buf, sizeof buf, "nm_half_tile_kernel<%dx%d,mi%d,wk%d>,stage%d,split%d", c.tile->BM, c.tile->BN,
-                  c.tile->MI, c.tile->WK, c.P * l.KR, c.splits);
+    const HalfTileInfo &t = half_tiles[c.tile];
+    std::snprintf(buf, sizeof buf, "nm_half_tile_kernel<%dx%d,mi%d,wk%d,qs%d>,stage%d,split%d", t.BM, t.BN, t.MI,
+                  t.WK, c.QS, c.P * l.KR, c.splits);
     return buf;
 }
 
@@ -439,10 +460,10 @@ extern "C" nmspmm_status_t nmspmm_half_run(const void *A, int64_t lda, const nms
                               rows16(C, ldc) && rows16(mul, ld_mul) && rows16(residual, ld_residual) &&
                                   aligned_to(bias, 16)};
     int cached = -1;
-    HalfPlan c = plan_for(m, l, w, lda, true);
+    HalfPlan c = plan_for(A, lda, m, l, w, true);
     if (c.ws_bytes > 0 && (!workspace || (uint64_t)c.ws_bytes > (uint64_t)workspace_bytes)) {
         workspace = capturing(stream) ? nullptr : ws_acquire(stream, (size_t)c.ws_bytes, &cached);
-        if (!workspace) c = plan_for(m, l, w, lda, false);
+        if (!workspace) c = plan_for(A, lda, m, l, w, false);
     }
     const hipError_t e = w.dtype == NMSPMM_BF16 ? run<bf16_t>(c, l, A, lda, w, m, epi, workspace, stream)
                                                 : run<f16_t>(c, l, A, lda, w, m, epi, workspace, stream);

@@ -14,11 +14,16 @@
 //         BM rows of C, 16 to a granule of 32 bytes; one last row of zeros is
 //         where padding offsets lead, so that no value of A meets a padding
 //         row's zero.  Global -> registers (4 rows x 8 columns a block) ->
-//         transposed by byte permutes -> LDS, one stage ahead, two slots.
+//         transposed by byte permutes -> LDS: two slots, and the slab after the
+//         next on its way to registers.
 //   gather: ds_read_b64_tr_b16 hands 16 lanes four LDS rows of 16 outputs,
 //         each row at its own address, already transposed into the A operand:
 //         the gather of Eq. 1 costs nothing beyond the read.
-//   B, offsets: straight from memory into registers, two operands ahead.
+//   B, offsets: straight from memory into registers, one stage ahead (a stage
+//         has a fixed number of operands a wave, QS, so that every wait counts
+//         the loads that are younger exactly; with a run-time number, each wait
+//         for B waited for the slab of A that had just been asked for as well:
+//         4096^3 at 16:32 170 us).
 // Granule g of row c lies at place g ^ swz(c), which spreads a transposed read
 // over the banks.  The WK waves of a tile share out the units of every stage
 // and are joined through LDS at the end.
@@ -46,7 +51,7 @@ struct HalfTileArgs {
     const uint16_t *offs;
     float *part;            // with split-k: splits x m x n partial sums
     int64_t lda, m, n, k;
-    int32_t V, S, KR, units, P, QS, nst;
+    int32_t V, S, KR, P, steps, nst;     // S operands a unit, P units a stage, `steps` operands a column tile
     int32_t tiles_m, tiles_n, splits;
     HalfEpilogue epi;
 };
@@ -79,36 +84,39 @@ struct HalfTile {
     static constexpr int STEP = 512 / MI, PITCH = 2 * BM, LDS_BYTES = 1024 * LDS_KB_;
     static constexpr int ACCS = RT * CT * NG;
     // waves a SIMD: two workgroups a CU where their LDS leaves room
-    static constexpr int WPS = NT / 256 * (LDS_KB_ <= 80 ? 2 : 1);
+    static constexpr int WPS = NT / 256 * (160 / LDS_KB_);
     static constexpr int RED_BYTES = WK > 1 ? (WK / 2) * WR * WC * ACCS * MI * MI * 4 : 0;
     static constexpr int CW = CT * NG * MI, CPITCH = CW + 4;        // a wave's columns
     static_assert((RT & (RT - 1)) == 0 && RED_BYTES <= LDS_BYTES && WR * WC * WK * MI * CPITCH * 4 <= LDS_BYTES &&
                       64 / (CW / 8) <= MI, "tile shape");
     // columns of A of a stage at most: by LDS (two slots with their row of zeros) and by registers
     static constexpr int KMAX_LDS = (LDS_BYTES / 2 / PITCH - 1) / 8 * 8;
-    static constexpr int KMAX_REG = NB * NT / BM * 4 * 8;
+    static constexpr int KMAX_REG = NB * NT / (2 * BM) * 64;
     static constexpr int KMAX = KMAX_LDS < KMAX_REG ? KMAX_LDS : KMAX_REG;
-    // place of LDS row c's granules: consecutive rows on different banks
+    // What row c's granules are XORed with: the rows of a transposed read and
+    // the eight rows apart that a store writes at once lie on different banks.
     __device__ static constexpr int swz(int c)
     {
-        if (MI == 32) return BM >= 128 ? (c & 3) << 1 : BM == 64 ? c & 2 : 0;
-        return BM >= 128 ? c & 7 : BM == 64 ? (c >> 1) & 3 : BM == 32 ? (c >> 2) & 1 : 0;
+        const int x = c ^ (c >> 3);
+        return BM >= 128 ? x & 7 : BM == 64 ? ((c >> 1) ^ (c >> 3)) & 3 : BM == 32 ? ((c >> 2) ^ (c >> 3)) & 1 : 0;
     }
 };
 
-// Rows 4 x columns 8 of 16-bit values, transposed: out[j] holds column j.
-__device__ __forceinline__ void transpose_4x8(const u32x4 (&r)[4], u32x2 (&out)[8])
+// Columns 4*half .. 4*half+3 of 4 rows x 8 columns of 16-bit values: out[j]
+// holds column 4*half + j.
+__device__ __forceinline__ void transpose_4x4(const u32x4 (&r)[4], int half, u32x2 (&out)[4])
 {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        out[2 * j] = u32x2{__builtin_amdgcn_perm(r[1][j], r[0][j], 0x05040100u),
-                           __builtin_amdgcn_perm(r[3][j], r[2][j], 0x05040100u)};
-        out[2 * j + 1] = u32x2{__builtin_amdgcn_perm(r[1][j], r[0][j], 0x07060302u),
-                               __builtin_amdgcn_perm(r[3][j], r[2][j], 0x07060302u)};
+    for (int j = 0; j < 2; ++j) {
+        const int w = 2 * half + j;
+        out[2 * j] = u32x2{__builtin_amdgcn_perm(r[1][w], r[0][w], 0x05040100u),
+                           __builtin_amdgcn_perm(r[3][w], r[2][w], 0x05040100u)};
+        out[2 * j + 1] = u32x2{__builtin_amdgcn_perm(r[1][w], r[0][w], 0x07060302u),
+                               __builtin_amdgcn_perm(r[3][w], r[2][w], 0x07060302u)};
     }
 }
 
-template <class T, class C, bool VEC>
+template <class T, class C, int QS, bool VEC>
 __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArgs p)
 {
     constexpr int MI = C::MI, CT = C::CT, NG = C::NG, RT = C::RT, WR = C::WR, WC = C::WC, WK = C::WK, NB = C::NB;
@@ -134,86 +142,69 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
                                                     (uint32_t)(((rows_valid - 1) * p.lda + p.k) * 2));
     u32x4 ra[NB][4];
     // block b of this thread: rows 4*rb.., columns 8*kc.. of the stage
-    auto block_rb = [&](int b) { return ((tid + b * NT) >> 2) % (BM / 4); };
-    auto block_kc = [&](int b) { return (tid & 3) + 4 * ((tid + b * NT) / BM); };
-    auto load_a = [&](int st) {
+    // (eight lanes to a row: whole 128-byte lines of A; halves of lines in
+    // different instructions waited for each other in L1)
+    auto block_rb = [&](int b) { return ((tid + b * NT) >> 3) % (BM / 4); };
+    auto block_kc = [&](int b) { return (tid & 7) + 8 * ((tid + b * NT) / (2 * BM)); };
+    auto load_a = [&](int b, int st, bool wanted) {
+        const int rb = block_rb(b), kc = block_kc(b);
+        const int64_t kpos = (int64_t)st * kstage + 8 * kc;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int rb = block_rb(b), kc = block_kc(b);
-            const int64_t kpos = (int64_t)st * kstage + 8 * kc;
+        for (int r = 0; r < 4; ++r) {
+            const bool ok = wanted && kc < chunks && 4 * rb + r < rows_valid && kpos < p.k;
+            const uint32_t off = (uint32_t)(((4 * rb + r) * p.lda + kpos) * 2);
+            if constexpr (VEC) {
+                ra[b][r] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, (int)(ok ? off : OOB), 0, 0));
+            } else {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const bool ok = kc < chunks && 4 * rb + r < rows_valid && kpos < p.k;
-                const uint32_t off = (uint32_t)(((4 * rb + r) * p.lda + kpos) * 2);
-                if constexpr (VEC) {
-                    ra[b][r] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, (int)(ok ? off : OOB), 0, 0));
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(ok ? off + 4 * j : OOB), 0, 0);
-                        const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(ok ? off + 4 * j + 2 : OOB), 0, 0);
-                        ra[b][r][j] = (lo & 0xffffu) | hi << 16;
-                    }
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(ok ? off + 4 * j : OOB), 0, 0);
+                    const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(ok ? off + 4 * j + 2 : OOB), 0, 0);
+                    ra[b][r][j] = (lo & 0xffffu) | hi << 16;
                 }
             }
         }
     };
-    auto store_a = [&](int slot) {
+    // half a block: four columns
+    auto store_a = [&](int b, int half, int slot) {
+        const int rb = block_rb(b), kc = block_kc(b);
+        if (kc < chunks) {
+            u32x2 col[4];
+            transpose_4x4(ra[b], half, col);
+            unsigned char *dst = lds + slot * slot_bytes + kc * 8 * PITCH;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int rb = block_rb(b), kc = block_kc(b);
-            if (kc < chunks) {
-                u32x2 col[8];
-                transpose_4x8(ra[b], col);
-                unsigned char *dst = lds + slot * slot_bytes + kc * 8 * PITCH;
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<u32x2 *>(dst + j * PITCH + (((rb >> 2) ^ C::swz(j)) << 5) + 8 * (rb & 3)) = col[j];
-            }
+            for (int j = 4 * half; j < 4 * half + 4; ++j)
+                *reinterpret_cast<u32x2 *>(dst + j * PITCH + (((rb >> 2) ^ C::swz(8 * kc) ^ C::swz(j)) << 5) + 8 * (rb & 3)) = col[j - 4 * half];
         }
     };
 
-    // ---- B operands and offsets, two steps ahead ----
-    const int nsteps = p.units * p.S;
+    // ---- B operands and offsets, one stage ahead: a wave takes QS steps in a
+    // row of every stage.  Past a tile's last operand the loads read zeros,
+    // and the offsets those of padding ----
     const uint32_t ctiles = (uint32_t)(p.n / MI);
-    const unsigned char *bp[NG][CT];
+    __amdgpu_buffer_rsrc_t b_rsrc[NG][CT];
     const unsigned char *op[NG];
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
         const uint32_t first = (uint32_t)(col0 / MI) + (wc * NG + g) * CT;
 #pragma unroll
         for (int c = 0; c < CT; ++c)
-            bp[g][c] = p.vals + (int64_t)min(first + c, ctiles - 1) * nsteps * 1024;
-        op[g] = reinterpret_cast<const unsigned char *>(p.offs) + (int64_t)(min(first, ctiles - 1) * MI / p.V) * nsteps * (2 * STEP);
+            b_rsrc[g][c] = make_rsrc(p.vals + (int64_t)min(first + c, ctiles - 1) * p.steps * 1024,
+                                     (uint32_t)p.steps * 1024);
+        op[g] = reinterpret_cast<const unsigned char *>(p.offs) +
+                (int64_t)(min(first, ctiles - 1) * MI / p.V) * (p.steps + 1) * (2 * STEP);
     }
-    const int pair = (lane / MI) * 4 + ((lane >> 2) & 3);
-    s16x8 rb_[2][NG][CT];
-    uint32_t ro[2][NG];
-    // a wave's steps in order: QS consecutive ones of every stage
-    struct Cursor {
-        int q, s, rows, step;
-    };
-    const int PW = p.P / WK;
-    auto advance = [&](Cursor &c) {
-        ++c.step;
-        if (++c.s == p.S) {
-            c.s = 0;
-            c.rows += p.KR;
-        }
-        if (++c.q == p.QS) {
-            c.q = 0;
-            c.rows = wk * PW * p.KR;
-            c.step += p.P * p.S - p.QS;
-        }
-    };
-    auto load_b = [&](int i, const Cursor &c) {
-        const int step = min(c.step, nsteps - 1);
+    const uint32_t pair = ((lane / MI) * 4 + ((lane >> 2) & 3)) * 4;
+    s16x8 rb_[QS][NG][CT];
+    uint32_t ro[QS][NG];
+    auto load_b = [&](int i, int st) {
+        const uint32_t step = (uint32_t)(st * p.P * p.S + wk * QS + i);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
+            ro[i][g] = *reinterpret_cast<const uint32_t *>(op[g] + min(step, (uint32_t)p.steps) * (2 * STEP) + pair);
 #pragma unroll
             for (int t = 0; t < CT; ++t)
-                rb_[i][g][t] = *reinterpret_cast<const s16x8 *>(bp[g][t] + (int64_t)step * 1024 + lane * 16);
-            ro[i][g] = *reinterpret_cast<const uint32_t *>(op[g] + (int64_t)step * (2 * STEP) + pair * 4);
+                rb_[i][g][t] = __builtin_bit_cast(s16x8, __builtin_amdgcn_raw_buffer_load_b128(b_rsrc[g][t], (int)(step * 1024 + lane * 16), 0, 0));
         }
     };
 
@@ -227,20 +218,21 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
 #pragma unroll
                 for (int e = 0; e < E; ++e) acc[g][t][c][e] = 0.f;
 
-    // where a lane of a transposed read looks: its piece of 4 outputs, and (MI
-    // = 32) its granule of the pair
-    const int piece = 8 * (lane & 3) + (MI == 32 ? 32 * ((lane >> 4) & 1) : 0);
+    // where a lane of a transposed read looks: its piece of 4 outputs in its
+    // granule (MI = 32: of a pair)
+    const int piece = 8 * (lane & 3);
     constexpr int TSHIFT = MI == 32 ? 6 : 5;
-    const int g0 = wr * RT << TSHIFT;
+    const int g0 = (wr * RT << TSHIFT) + (MI == 32 ? 32 * ((lane >> 4) & 1) : 0);
 
-    auto compute = [&](int i, const Cursor &c, uint32_t slot) {
+    auto compute = [&](int i, uint32_t slot) {
+        const uint32_t rows = (uint32_t)(wk * QS + i) / (uint32_t)p.S * p.KR;   // where the step's unit starts
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             uint32_t at[2];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const uint32_t off = x == 0 ? ro[i][g] & 0xffffu : ro[i][g] >> 16;
-                const uint32_t row = min(off + (uint32_t)c.rows, (uint32_t)zero_row);
+                const uint32_t row = min(off + rows, (uint32_t)zero_row);
                 at[x] = slot + row * PITCH + (g0 ^ (C::swz(row) << 5)) + piece;
             }
 #pragma unroll
@@ -261,36 +253,35 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
         // the rows of zeros of both slots
         for (int i = tid; i < 2 * (PITCH / 4); i += NT)
             *reinterpret_cast<uint32_t *>(lds + i / (PITCH / 4) * slot_bytes + zero_row * PITCH + i % (PITCH / 4) * 4) = 0;
-        load_a(s_begin);
-        Cursor use{0, 0, wk * PW * p.KR, (s_begin * p.P + wk * PW) * p.S}, ahead = use;
-        load_b(0, ahead);
-        advance(ahead);
-        load_b(1, ahead);
-        advance(ahead);
-        store_a(0);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) load_a(b, s_begin, true);
+#pragma unroll
+        for (int i = 0; i < QS; ++i) load_b(i, s_begin);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            store_a(b, 0, 0);
+            store_a(b, 1, 0);
+            load_a(b, s_begin + 1, s_begin + 1 < s_end);
+        }
         lds_sync();
-        if (s_begin + 1 < s_end) load_a(s_begin + 1);
-        int st = s_begin, slot = 0;
-        auto step = [&](int i) {
-            if (use.step < nsteps) compute(i, use, lds0 + slot * slot_bytes);
-            load_b(i, ahead);
-            advance(ahead);
-            advance(use);
-            if (use.q == 0) {
-                ++st;
-                slot ^= 1;
-                if (st < s_end) {
-                    store_a(slot);
-                    lds_sync();
-                    if (st + 1 < s_end) load_a(st + 1);
+        int slot = 0;
+        for (int st = s_begin; st < s_end; ++st) {
+            // the next stage's slab, which has been on its way for a stage, is
+            // written a part a step, and each block's registers take the one
+            // after
+#pragma unroll
+            for (int i = 0; i < QS; ++i) {
+#pragma unroll
+                for (int part = i * 2 * NB / QS; part < (i + 1) * 2 * NB / QS; ++part) {
+                    store_a(part / 2, part % 2, slot ^ 1);
+                    if (part % 2) load_a(part / 2, st + 2, st + 2 < s_end);
                 }
+                compute(i, lds0 + slot * slot_bytes);
+                load_b(i, st + 1);
+                __builtin_amdgcn_sched_barrier(0);
             }
-        };
-        while (true) {
-            step(0);
-            if (st >= s_end) break;
-            step(1);
-            if (st >= s_end) break;
+            slot ^= 1;
+            lds_sync();
         }
     }
 

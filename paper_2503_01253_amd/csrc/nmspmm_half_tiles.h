@@ -1,4 +1,4 @@
-// Host-side list of the tiled kernel's instantiations.
+// Host-side list of the tiled kernel's shapes.
 #ifndef NMSPMM_HALF_TILES_H
 #define NMSPMM_HALF_TILES_H
 
@@ -8,15 +8,32 @@ namespace nmspmm {
 
 struct HalfTileArgs;
 
-struct HalfTileInfo {
-    int MI, CT, WK, BM, BN, kmax;
-    hipError_t (*launch)(const HalfTileArgs &a, bool bf16, bool vec, hipStream_t stream);
-};
+// X(MI, CT, NG, RT, WR, WC, WK, NB, LDS KB, loads that need no alignment too)
+#define NMSPMM_HALF_TILES(X)                                \
+    X(32, 1, 1, 8, 1, 8, 1, 2, 160, 0)  /* 256 x 256 */     \
+    X(32, 1, 1, 4, 1, 4, 1, 2, 80, 0)   /* 128 x 128 */     \
+    X(32, 1, 1, 2, 1, 4, 2, 1, 80, 0)   /* 64 x 128 */      \
+    X(32, 1, 1, 2, 1, 2, 4, 1, 80, 1)   /* 64 x 64 */       \
+    X(32, 1, 1, 1, 1, 2, 4, 1, 80, 0)   /* 32 x 64 */       \
+    X(32, 1, 1, 1, 1, 1, 8, 1, 80, 0)   /* 32 x 32 */       \
+    X(32, 2, 1, 4, 2, 4, 1, 2, 160, 0)  /* 256 x 256 */     \
+    X(32, 2, 1, 2, 2, 2, 1, 2, 80, 0)   /* 128 x 128 */     \
+    X(32, 2, 1, 2, 1, 2, 2, 2, 80, 0)   /* 64 x 128 */      \
+    X(32, 2, 1, 2, 1, 1, 4, 2, 80, 0)   /* 64 x 64 */       \
+    X(32, 2, 1, 1, 1, 1, 8, 1, 80, 0)   /* 32 x 64 */       \
+    X(16, 1, 2, 16, 1, 8, 1, 2, 160, 0) /* 256 x 256 */     \
+    X(16, 1, 2, 8, 1, 4, 1, 2, 80, 0)   /* 128 x 128 */     \
+    X(16, 1, 2, 4, 1, 2, 4, 1, 80, 1)   /* 64 x 64 */       \
+    X(16, 1, 2, 2, 1, 1, 8, 1, 80, 0)   /* 32 x 32 */
 
-// one list per matrix-instruction shape and columns of a gather
-const HalfTileInfo *half_tiles_32x1(int *count);
-const HalfTileInfo *half_tiles_32x2(int *count);
-const HalfTileInfo *half_tiles_16(int *count);
+// A stage of 1 to 4 operands a wave.
+constexpr int HALF_MAX_QS = 4;
+
+// Launches tile `tile` of the list above with stages of QS operands a wave, one unit each.
+hipError_t launch_half_q1(int tile, const HalfTileArgs &a, bool bf16, bool vec, hipStream_t stream);
+hipError_t launch_half_q2(int tile, const HalfTileArgs &a, bool bf16, bool vec, hipStream_t stream);
+hipError_t launch_half_q3(int tile, const HalfTileArgs &a, bool bf16, bool vec, hipStream_t stream);
+hipError_t launch_half_q4(int tile, const HalfTileArgs &a, bool bf16, bool vec, hipStream_t stream);
 
 }  // namespace nmspmm
 
