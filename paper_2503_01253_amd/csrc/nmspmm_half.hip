@@ -24,13 +24,11 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // Where V is a multiple of 16 the values lie as the matrix instruction reads
 // them (nmspmm_half_tile.h): MI columns by STEP compressed rows an operand, a
 // column tile's operands in the order of its units and steps; the offsets lie
-// in the same order, one per block and compressed row, as 16-bit columns of
-// the unit (PAD in padding rows), rows u and u + 4 of each eight side by side,
-// which is how a lane reads them, and a block's end with a step of padding.
-// Other widths, and windows of so many kept rows that no stage holds them,
-// keep Bc and idx as they are (MI = 0).
-constexpr uint16_t PAD = 0xffff;
-
+// in the same order, one per block and compressed row: the column c of the
+// unit as c * 8 + half_swz(c), or KR * 8 in padding rows; rows u and u + 4 of
+// each eight lie side by side, which is how a lane reads them, and a block's
+// end with a step of padding.  Other widths, and windows too long or of too
+// many kept rows for a stage, keep Bc and idx as they are (MI = 0).
 struct HalfLayout {
     int MI, STEP, G, S, KR;
     int64_t w, q, windows, units, steps;    // units and steps of a column tile
@@ -43,27 +41,28 @@ HalfLayout half_layout(int64_t k, int64_t n, int N, int M, int V)
     l.windows = k / M;
     l.w = l.windows * N;
     l.q = n / V;
-    if (V % 16 || N > HALF_MAX_QS * (V % 32 ? 32 : 16)) {
-        l.offs_at = round_up(2 * l.w * n, 256);
-        l.bytes = l.offs_at + l.w * l.q;
-        return l;
-    }
-    l.MI = V % 32 ? 16 : 32;
-    l.STEP = 512 / l.MI;
-    // the fewest windows whose rows fill their operands best, within 128
-    // columns of A (which bound the LDS a stage takes) and the operands of a
-    // stage
+    // the fewest windows whose rows fill their operands best: whole pieces of 8
+    // columns, at most 128 (which bound the LDS a stage takes), and the operands
+    // of a stage
+    const int MI = V % 16 ? 0 : V % 32 ? 16 : 32;
     double best = 0;
-    for (int G = 1; G == 1 || G * M <= 128; ++G) {
-        const int S = (G * N + l.STEP - 1) / l.STEP;
+    for (int G = 1; MI && G * M <= 128; ++G) {
+        const int step = 512 / MI, S = (G * N + step - 1) / step;
         if (S > HALF_MAX_QS) break;
-        const double fill = (double)(G * N) / (S * l.STEP);
-        if (fill > best + 1e-9) {
+        const double fill = (double)(G * N) / (S * step);
+        if (G * M % 8 == 0 && fill > best + 1e-9) {
             best = fill;
             l.G = G;
             l.S = S;
         }
     }
+    if (l.G == 0) {
+        l.offs_at = round_up(2 * l.w * n, 256);
+        l.bytes = l.offs_at + l.w * l.q;
+        return l;
+    }
+    l.MI = MI;
+    l.STEP = 512 / MI;
     l.KR = l.G * M;
     l.units = (l.windows + l.G - 1) / l.G;
     l.steps = l.units * l.S;
@@ -127,7 +126,8 @@ __global__ __launch_bounds__(256) void nm_half_pack_kernel(PackArgs p)
         int win;
         const int64_t u = packed_row(p, unit, slot, win);
         const int o = u < 0 ? 0 : p.idx[u * p.l.q + block];
-        p.offs[e] = u < 0 ? PAD : (uint16_t)(win * p.M + (o < p.M ? o : p.M - 1));
+        const int c = win * p.M + (o < p.M ? o : p.M - 1);
+        p.offs[e] = u < 0 ? p.l.KR * 8 : c * 8 + half_swz(c);
     }
 }
 
@@ -178,8 +178,8 @@ __global__ __launch_bounds__(256) void nm_half_general_kernel(GeneralArgs p)
             for (int64_t step = 0; step < p.l.steps; ++step)
                 for (int u = 0; u < p.l.STEP; ++u) {
                     const uint16_t o = offs[step * p.l.STEP + u / 8 * 8 + u % 4 * 2 + u % 8 / 4];
-                    if (o != PAD)
-                        add(step / p.l.S * p.l.KR + o, to_f32(tile[(step * 64 + u / 8 * p.l.MI) * 8 + u % 8]));
+                    if (o / 8 < p.l.KR)
+                        add(step / p.l.S * p.l.KR + o / 8, to_f32(tile[(step * 64 + u / 8 * p.l.MI) * 8 + u % 8]));
                 }
         }
 #pragma unroll
@@ -214,13 +214,14 @@ __global__ __launch_bounds__(256) void nm_half_join_kernel(const float *part, in
 }
 
 struct HalfTileInfo {
-    int MI, CT, WK, BM, BN, NT, kmax, per_cu;
+    int MI, CT, WK, BM, BN, NT, kmax, rows, per_cu;
     bool any;       // takes any alignment of A
 };
 
 #define NMSPMM_HALF_INFO(MI, CT, NG, RT, WR, WC, WK, NB, LDS, ANY)                                               \
     {MI, CT, WK, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::BM, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::BN, \
-     HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::NT, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::KMAX, 160 / LDS, \
+     HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::NT, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::KMAX, \
+     HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::ROWS, 160 / LDS, \
      ANY != 0},
 const HalfTileInfo half_tiles[] = {NMSPMM_HALF_TILES(NMSPMM_HALF_INFO)};
 #undef NMSPMM_HALF_INFO
@@ -237,7 +238,7 @@ struct HalfPlan {
 // larger of a tile's matrix work, its LDS traffic and what it loads from L2.
 double half_cost(const HalfTileInfo &t, const HalfLayout &l, int64_t tiles)
 {
-    const double rounds = (double)((tiles + 255) / 256);
+    const double rounds = (double)((tiles + 511) / 512) * 2;
     const double slots = (double)l.units * l.S * l.STEP, cols = (double)l.units * l.KR;
     const double mfma = 2.0 * t.BM * t.BN * slots / 4096;
     const double lds = (slots * t.BM * 2 * (t.BN / (t.CT * t.MI)) + cols * t.BM * 2) / 100;
@@ -249,7 +250,7 @@ double half_cost(const HalfTileInfo &t, const HalfLayout &l, int64_t tiles)
 HalfPlan half_plan(int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w, bool vec, bool may_split)
 {
     HalfPlan best;
-    if (l.MI == 0 || w.k == 0 || w.k >= (int64_t)1 << 22) return best;
+    if (l.MI == 0 || w.k == 0 || w.k >= (int64_t)1 << 21) return best;
     double best_cost = 1e300;
     for (int i = 0; i < half_tile_count; ++i) {
         const HalfTileInfo &t = half_tiles[i];
@@ -258,10 +259,10 @@ HalfPlan half_plan(int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w
         c.tile = i;
         // the longest stage that LDS and registers hold
         for (int QS = HALF_MAX_QS; QS >= 1 && c.QS == 0; --QS)
-            if (QS % l.S == 0 && QS / l.S * t.WK * l.KR <= t.kmax) c.QS = QS;
+            if (QS % l.S == 0 && QS / l.S * t.WK * l.KR <= t.kmax && QS / l.S * t.WK * (l.KR + 1) <= t.rows) c.QS = QS;
         if (c.QS == 0) continue;
         c.P = c.QS / l.S * t.WK;
-        c.vec = vec && c.P * l.KR % 8 == 0;
+        c.vec = vec;
         if (!c.vec && !t.any) continue;
         if (w.V % (t.CT * t.MI)) continue;
         const int64_t tiles_m = (m + t.BM - 1) / t.BM, tiles_n = (w.n + t.BN - 1) / t.BN;
@@ -377,11 +378,11 @@ hipError_t run(const HalfPlan &c, const HalfLayout &l, const void *A, int64_t ld
 }
 
 // The plan of a call.  Where a row of A lies so far from the next that a
-// tile's rows span 2^31 bytes, the general kernel runs.
+// tile's rows span 2^29 bytes, the general kernel runs.
 HalfPlan plan_for(const void *A, int64_t lda, int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w,
                   bool may_split)
 {
-    if (lda >= (int64_t)1 << 22) return HalfPlan{};
+    if (lda >= (int64_t)1 << 21) return HalfPlan{};
     return half_plan(m, l, w, aligned_to(A, 16) && (m == 1 || lda % 8 == 0), may_split);
 }
 

@@ -11,11 +11,11 @@
 // A workgroup of WR x WC x WK waves owns BM x BN outputs (and, with split-k,
 // one slice of k).  It walks k in stages of P units:
 //   A_s : the BM x P*KR slab of A in LDS, k-major: row c holds column c of A,
-//         BM rows of C, 16 to a granule of 32 bytes; one last row of zeros is
-//         where padding offsets lead, so that no value of A meets a padding
-//         row's zero.  Global -> registers (4 rows x 8 columns a block) ->
-//         transposed by byte permutes -> LDS: two slots, and the slab after the
-//         next on its way to registers.
+//         BM rows of C, 16 to a granule of 32 bytes; after every unit one row
+//         of zeros, where padding offsets lead, so that no value of A meets a
+//         padding row's zero.  Global -> registers (4 rows x 8 columns a
+//         block) -> transposed by byte permutes -> LDS: two slots, and the
+//         slab after the next on its way to registers.
 //   gather: ds_read_b64_tr_b16 hands 16 lanes four LDS rows of 16 outputs,
 //         each row at its own address, already transposed into the A operand:
 //         the gather of Eq. 1 costs nothing beyond the read.
@@ -23,10 +23,11 @@
 //         has a fixed number of operands a wave, QS, so that every wait counts
 //         the loads that are younger exactly; with a run-time number, each wait
 //         for B waited for the slab of A that had just been asked for as well:
-//         4096^3 at 16:32 170 us).
-// Granule g of row c lies at place g ^ swz(c), which spreads a transposed read
-// over the banks.  The WK waves of a tile share out the units of every stage
-// and are joined through LDS at the end.
+//         4096^3 at 16:32 174 us, with fixed stages 151).
+// Granule g of a unit's row c lies at place g ^ swz(c), which spreads reads and
+// writes over the banks; the packed offset holds swz(c) beside c, so that a
+// lane forms its address with four instructions.  The WK waves of a tile share
+// out the units of every stage and are joined through LDS at the end.
 #ifndef NMSPMM_HALF_TILE_H
 #define NMSPMM_HALF_TILE_H
 
@@ -81,26 +82,24 @@ template <int MI_, int CT_, int NG_, int RT_, int WR_, int WC_, int WK_, int NB_
 struct HalfTile {
     static constexpr int MI = MI_, CT = CT_, NG = NG_, RT = RT_, WR = WR_, WC = WC_, WK = WK_, NB = NB_;
     static constexpr int BM = MI * RT * WR, BN = MI * CT * NG * WC, NT = 64 * WR * WC * WK;
-    static constexpr int STEP = 512 / MI, PITCH = 2 * BM, LDS_BYTES = 1024 * LDS_KB_;
+    static constexpr int STEP = 512 / MI, PSHIFT = BM == 128 ? 8 : BM == 64 ? 7 : 6, PITCH = 1 << PSHIFT,
+                         LDS_BYTES = 1024 * LDS_KB_;
     static constexpr int ACCS = RT * CT * NG;
     // waves a SIMD: two workgroups a CU where their LDS leaves room
     static constexpr int WPS = NT / 256 * (160 / LDS_KB_);
     static constexpr int RED_BYTES = WK > 1 ? (WK / 2) * WR * WC * ACCS * MI * MI * 4 : 0;
     static constexpr int CW = CT * NG * MI, CPITCH = CW + 4;        // a wave's columns
-    static_assert((RT & (RT - 1)) == 0 && RED_BYTES <= LDS_BYTES && WR * WC * WK * MI * CPITCH * 4 <= LDS_BYTES &&
+    static_assert((RT & (RT - 1)) == 0 && PITCH == 2 * BM && RED_BYTES <= LDS_BYTES && WR * WC * WK * MI * CPITCH * 4 <= LDS_BYTES &&
                       64 / (CW / 8) <= MI, "tile shape");
-    // columns of A of a stage at most: by LDS (two slots with their row of zeros) and by registers
-    static constexpr int KMAX_LDS = (LDS_BYTES / 2 / PITCH - 1) / 8 * 8;
-    static constexpr int KMAX_REG = NB * NT / (2 * BM) * 64;
-    static constexpr int KMAX = KMAX_LDS < KMAX_REG ? KMAX_LDS : KMAX_REG;
-    // What row c's granules are XORed with: the rows of a transposed read and
-    // the eight rows apart that a store writes at once lie on different banks.
-    __device__ static constexpr int swz(int c)
-    {
-        const int x = c ^ (c >> 3);
-        return BM >= 128 ? x & 7 : BM == 64 ? ((c >> 1) ^ (c >> 3)) & 3 : BM == 32 ? ((c >> 2) ^ (c >> 3)) & 1 : 0;
-    }
+    // rows of a slot, and columns of A of a stage, at most
+    static constexpr int ROWS = LDS_BYTES / 2 / PITCH, KMAX = NB * NT / (2 * BM) * 64;
+    // the bits of swz(c) that a row of BM outputs has room for
+    static constexpr int SWZ = BM / 16 - 1 < 7 ? BM / 16 - 1 : 7;
 };
+
+// What the granules of a unit's row c are XORed with: rows next to each other
+// (of a transposed read) and rows 8 apart (of a write) lie on different banks.
+__host__ __device__ constexpr int half_swz(int c) { return (c ^ (c >> 3)) & 7; }
 
 // Columns 4*half .. 4*half+3 of 4 rows x 8 columns of 16-bit values: out[j]
 // holds column 4*half + j.
@@ -135,31 +134,38 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
     const int s_begin = split * sps, s_end = min(p.nst, s_begin + sps);
 
     // ---- A: global -> registers -> LDS ----
-    const int kstage = p.P * p.KR, chunks = (kstage + 7) / 8, zero_row = chunks * 8;
-    const int slot_bytes = (zero_row + 1) * PITCH;
+    const int kstage = p.P * p.KR, slot_bytes = p.P * (p.KR + 1) * PITCH;
     const int rows_valid = (int)min64(BM, p.m - row0);
+    // (rows past the last and columns past k read zeros or a neighbour's
+    // values: the former's outputs are not stored, no offset leads to the latter)
     const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(static_cast<const T *>(p.A) + row0 * p.lda,
                                                     (uint32_t)(((rows_valid - 1) * p.lda + p.k) * 2));
     u32x4 ra[NB][4];
-    // block b of this thread: rows 4*rb.., columns 8*kc.. of the stage
-    // (eight lanes to a row: whole 128-byte lines of A; halves of lines in
-    // different instructions waited for each other in L1)
-    auto block_rb = [&](int b) { return ((tid + b * NT) >> 3) % (BM / 4); };
-    auto block_kc = [&](int b) { return (tid & 7) + 8 * ((tid + b * NT) / (2 * BM)); };
-    auto load_a = [&](int b, int st, bool wanted) {
-        const int rb = block_rb(b), kc = block_kc(b);
-        const int64_t kpos = (int64_t)st * kstage + 8 * kc;
+    uint32_t a_off[NB], a_dst[NB];
+    // block b of this thread: rows 4*rb.., columns 8*kc.. of the stage (eight
+    // lanes to a row: whole 128-byte lines of A; halves of lines in different
+    // instructions waited for each other in L1)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int rb = ((tid + b * NT) >> 3) % (BM / 4), kc = (tid & 7) + 8 * ((tid + b * NT) / (2 * BM));
+        const int unit = 8 * kc / p.KR, c = 8 * kc - unit * p.KR;
+        a_off[b] = 8 * kc < kstage ? (uint32_t)((4 * rb * p.lda + 8 * kc) * 2) : OOB;
+        a_dst[b] = 8 * kc < kstage ? (uint32_t)((unit * (p.KR + 1) + c) * PITCH +
+                                                (((rb >> 2) ^ (half_swz(c) & C::SWZ)) << 5) + 8 * (rb & 3)) : OOB;
+    }
+    constexpr int PAST = 0x40000000;    // past every tile's rows of A (under 2^29 bytes), and no overflow beside OOB
+    auto load_a = [&](int b, int st) {
+        const int at = st < s_end ? st * kstage * 2 : PAST;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const bool ok = wanted && kc < chunks && 4 * rb + r < rows_valid && kpos < p.k;
-            const uint32_t off = (uint32_t)(((4 * rb + r) * p.lda + kpos) * 2);
+            const uint32_t off = a_off[b] + (uint32_t)(r * p.lda * 2);
             if constexpr (VEC) {
-                ra[b][r] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, (int)(ok ? off : OOB), 0, 0));
+                ra[b][r] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, (int)a_off[b], (int)(at + r * (int)p.lda * 2), 0));
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(ok ? off + 4 * j : OOB), 0, 0);
-                    const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(ok ? off + 4 * j + 2 : OOB), 0, 0);
+                    const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(off + 4 * j), at, 0);
+                    const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(off + 4 * j + 2), at, 0);
                     ra[b][r][j] = (lo & 0xffffu) | hi << 16;
                 }
             }
@@ -167,14 +173,13 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
     };
     // half a block: four columns
     auto store_a = [&](int b, int half, int slot) {
-        const int rb = block_rb(b), kc = block_kc(b);
-        if (kc < chunks) {
-            u32x2 col[4];
-            transpose_4x4(ra[b], half, col);
-            unsigned char *dst = lds + slot * slot_bytes + kc * 8 * PITCH;
+        u32x2 col[4];
+        transpose_4x4(ra[b], half, col);
+        if (a_dst[b] != OOB) {
+            unsigned char *dst = lds + slot * slot_bytes;
 #pragma unroll
             for (int j = 4 * half; j < 4 * half + 4; ++j)
-                *reinterpret_cast<u32x2 *>(dst + j * PITCH + (((rb >> 2) ^ C::swz(8 * kc) ^ C::swz(j)) << 5) + 8 * (rb & 3)) = col[j - 4 * half];
+                *reinterpret_cast<u32x2 *>(dst + j * PITCH + (a_dst[b] ^ ((j & C::SWZ) << 5))) = col[j - 4 * half];
         }
     };
 
@@ -225,15 +230,15 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
     const int g0 = (wr * RT << TSHIFT) + (MI == 32 ? 32 * ((lane >> 4) & 1) : 0);
 
     auto compute = [&](int i, uint32_t slot) {
-        const uint32_t rows = (uint32_t)(wk * QS + i) / (uint32_t)p.S * p.KR;   // where the step's unit starts
+        const uint32_t base = slot + (uint32_t)(wk * QS + i) / (uint32_t)p.S * (p.KR + 1) * PITCH;  // the step's unit
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
             uint32_t at[2];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const uint32_t off = x == 0 ? ro[i][g] & 0xffffu : ro[i][g] >> 16;
-                const uint32_t row = min(off + rows, (uint32_t)zero_row);
-                at[x] = slot + row * PITCH + (g0 ^ (C::swz(row) << 5)) + piece;
+                const uint32_t v = x == 0 ? ro[i][g] & 0xffffu : ro[i][g] >> 16;    // row * 8 + swz(row)
+                const uint32_t place = PITCH == 256 ? v << 5 : (v >> 3 << C::PSHIFT) + ((v & C::SWZ) << 5);
+                at[x] = (place ^ (g0 + piece)) + base;
             }
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
@@ -250,18 +255,20 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_u8 *)(lds_void *)lds;
     if (s_begin < s_end) {
-        // the rows of zeros of both slots
-        for (int i = tid; i < 2 * (PITCH / 4); i += NT)
-            *reinterpret_cast<uint32_t *>(lds + i / (PITCH / 4) * slot_bytes + zero_row * PITCH + i % (PITCH / 4) * 4) = 0;
+        // the rows of zeros of both slots' units
+        for (int i = tid; i < 2 * p.P * (PITCH / 4); i += NT) {
+            const int unit = i / (PITCH / 4);
+            *reinterpret_cast<uint32_t *>(lds + (unit * (p.KR + 1) + p.KR) * PITCH + i % (PITCH / 4) * 4) = 0;
+        }
 #pragma unroll
-        for (int b = 0; b < NB; ++b) load_a(b, s_begin, true);
+        for (int b = 0; b < NB; ++b) load_a(b, s_begin);
 #pragma unroll
         for (int i = 0; i < QS; ++i) load_b(i, s_begin);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             store_a(b, 0, 0);
             store_a(b, 1, 0);
-            load_a(b, s_begin + 1, s_begin + 1 < s_end);
+            load_a(b, s_begin + 1);
         }
         lds_sync();
         int slot = 0;
@@ -274,7 +281,7 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
 #pragma unroll
                 for (int part = i * 2 * NB / QS; part < (i + 1) * 2 * NB / QS; ++part) {
                     store_a(part / 2, part % 2, slot ^ 1);
-                    if (part % 2) load_a(part / 2, st + 2, st + 2 < s_end);
+                    if (part % 2) load_a(part / 2, st + 2);
                 }
                 compute(i, lds0 + slot * slot_bytes);
                 load_b(i, st + 1);
