@@ -218,10 +218,10 @@ struct HalfTileInfo {
     bool any;       // takes any alignment of A
 };
 
-#define NMSPMM_HALF_INFO(MI, CT, NG, RT, WR, WC, WK, NB, LDS, ANY)                                               \
-    {MI, CT, WK, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::BM, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::BN, \
-     HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::NT, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::KMAX, \
-     HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>::ROWS, 160 / LDS, \
+#define NMSPMM_HALF_INFO(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS, ANY)                                               \
+    {MI, CT, WK, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>::BM, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>::BN, \
+     HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>::NT, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>::KMAX, \
+     HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>::ROWS, 160 / LDS, \
      ANY != 0},
 const HalfTileInfo half_tiles[] = {NMSPMM_HALF_TILES(NMSPMM_HALF_INFO)};
 #undef NMSPMM_HALF_INFO

@@ -22,10 +22,10 @@ template <int QS>
 hipError_t launch_half(int tile, const HalfTileArgs &a, bool bf16, bool vec, hipStream_t stream)
 {
     int at = 0;
-#define NMSPMM_HALF_CASE(MI, CT, NG, RT, WR, WC, WK, NB, LDS, ANY)                                                   \
+#define NMSPMM_HALF_CASE(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS, ANY)                                                   \
     if (tile == at++)                                                                                                \
-        return bf16 ? launch_half_tile<bf16_t, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>, QS, ANY>(a, vec, stream) \
-                    : launch_half_tile<f16_t, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, LDS>, QS, ANY>(a, vec, stream);
+        return bf16 ? launch_half_tile<bf16_t, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>, QS, ANY>(a, vec, stream) \
+                    : launch_half_tile<f16_t, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>, QS, ANY>(a, vec, stream);
     NMSPMM_HALF_TILES(NMSPMM_HALF_CASE)
 #undef NMSPMM_HALF_CASE
     return hipErrorInvalidValue;

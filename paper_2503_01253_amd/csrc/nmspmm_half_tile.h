@@ -15,7 +15,7 @@
 //         of zeros, where padding offsets lead, so that no value of A meets a
 //         padding row's zero.  Global -> registers (4 rows x 8 columns a
 //         block) -> transposed by byte permutes -> LDS: two slots, and the
-//         slab after the next on its way to registers.
+//         AD slabs after them on their way to registers.
 //   gather: ds_read_b64_tr_b16 hands 16 lanes four LDS rows of 16 outputs,
 //         each row at its own address, already transposed into the A operand:
 //         the gather of Eq. 1 costs nothing beyond the read.
@@ -78,9 +78,9 @@ __device__ __forceinline__ typename MfmaAcc<MI>::type half_mfma(s16x8 a, s16x8 b
 // The shape of a tile: MI x MI accumulators, RT of them down a wave's rows and
 // CT across the columns of each of its NG gathers; NB blocks of A a thread
 // and stage; LDS_KB of LDS.
-template <int MI_, int CT_, int NG_, int RT_, int WR_, int WC_, int WK_, int NB_, int LDS_KB_>
+template <int MI_, int CT_, int NG_, int RT_, int WR_, int WC_, int WK_, int NB_, int AD_, int LDS_KB_>
 struct HalfTile {
-    static constexpr int MI = MI_, CT = CT_, NG = NG_, RT = RT_, WR = WR_, WC = WC_, WK = WK_, NB = NB_;
+    static constexpr int MI = MI_, CT = CT_, NG = NG_, RT = RT_, WR = WR_, WC = WC_, WK = WK_, NB = NB_, AD = AD_;
     static constexpr int BM = MI * RT * WR, BN = MI * CT * NG * WC, NT = 64 * WR * WC * WK;
     static constexpr int STEP = 512 / MI, PSHIFT = BM == 128 ? 8 : BM == 64 ? 7 : 6, PITCH = 1 << PSHIFT,
                          LDS_BYTES = 1024 * LDS_KB_;
@@ -118,7 +118,7 @@ __device__ __forceinline__ void transpose_4x4(const u32x4 (&r)[4], int half, u32
 template <class T, class C, int QS, bool VEC>
 __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArgs p)
 {
-    constexpr int MI = C::MI, CT = C::CT, NG = C::NG, RT = C::RT, WR = C::WR, WC = C::WC, WK = C::WK, NB = C::NB;
+    constexpr int MI = C::MI, CT = C::CT, NG = C::NG, RT = C::RT, WR = C::WR, WC = C::WC, WK = C::WK, NB = C::NB, AD = C::AD;
     constexpr int BM = C::BM, BN = C::BN, NT = C::NT, STEP = C::STEP, PITCH = C::PITCH;
     typedef typename MfmaAcc<MI>::type acc_t;
     constexpr int E = MfmaAcc<MI>::E;
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
     // values: the former's outputs are not stored, no offset leads to the latter)
     const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(static_cast<const T *>(p.A) + row0 * p.lda,
                                                     (uint32_t)(((rows_valid - 1) * p.lda + p.k) * 2));
-    u32x4 ra[NB][4];
+    u32x4 ra[AD][NB][4];
     uint32_t a_off[NB], a_dst[NB];
     // block b of this thread: rows 4*rb.., columns 8*kc.. of the stage (eight
     // lanes to a row: whole 128-byte lines of A; halves of lines in different
@@ -154,27 +154,27 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
                                                 (((rb >> 2) ^ (half_swz(c) & C::SWZ)) << 5) + 8 * (rb & 3)) : OOB;
     }
     constexpr int PAST = 0x40000000;    // past every tile's rows of A (under 2^29 bytes), and no overflow beside OOB
-    auto load_a = [&](int b, int st) {
+    auto load_a = [&](int d, int b, int st) {
         const int at = st < s_end ? st * kstage * 2 : PAST;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const uint32_t off = a_off[b] + (uint32_t)(r * p.lda * 2);
             if constexpr (VEC) {
-                ra[b][r] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, (int)a_off[b], (int)(at + r * (int)p.lda * 2), 0));
+                ra[d][b][r] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, (int)a_off[b], (int)(at + r * (int)p.lda * 2), 0));
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(off + 4 * j), at, 0);
                     const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(a_rsrc, (int)(off + 4 * j + 2), at, 0);
-                    ra[b][r][j] = (lo & 0xffffu) | hi << 16;
+                    ra[d][b][r][j] = (lo & 0xffffu) | hi << 16;
                 }
             }
         }
     };
     // half a block: four columns
-    auto store_a = [&](int b, int half, int slot) {
+    auto store_a = [&](int d, int b, int half, int slot) {
         u32x2 col[4];
-        transpose_4x4(ra[b], half, col);
+        transpose_4x4(ra[d][b], half, col);
         if (a_dst[b] != OOB) {
             unsigned char *dst = lds + slot * slot_bytes;
 #pragma unroll
@@ -261,34 +261,38 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
             *reinterpret_cast<uint32_t *>(lds + (unit * (p.KR + 1) + p.KR) * PITCH + i % (PITCH / 4) * 4) = 0;
         }
 #pragma unroll
-        for (int b = 0; b < NB; ++b) load_a(b, s_begin);
+        for (int b = 0; b < NB; ++b) load_a(0, b, s_begin);
 #pragma unroll
         for (int i = 0; i < QS; ++i) load_b(i, s_begin);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            store_a(b, 0, 0);
-            store_a(b, 1, 0);
-            load_a(b, s_begin + 1);
+            store_a(0, b, 0, 0);
+            store_a(0, b, 1, 0);
         }
+#pragma unroll
+        for (int d = 1; d <= AD; ++d)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) load_a(d % AD, b, s_begin + d);
         lds_sync();
-        int slot = 0;
-        for (int st = s_begin; st < s_end; ++st) {
-            // the next stage's slab, which has been on its way for a stage, is
-            // written a part a step, and each block's registers take the one
-            // after
+        // the next stage's slab, which has been on its way for AD stages, is
+        // written a part a step, and each block's registers take the one AD
+        // stages on
+        auto stage = [&](int st, int d, int slot) {
 #pragma unroll
             for (int i = 0; i < QS; ++i) {
 #pragma unroll
                 for (int part = i * 2 * NB / QS; part < (i + 1) * 2 * NB / QS; ++part) {
-                    store_a(part / 2, part % 2, slot ^ 1);
-                    if (part % 2) load_a(part / 2, st + 2);
+                    store_a(d, part / 2, part % 2, slot ^ 1);
+                    if (part % 2) load_a(d, part / 2, st + 1 + AD);
                 }
                 compute(i, lds0 + slot * slot_bytes);
                 load_b(i, st + 1);
-                __builtin_amdgcn_sched_barrier(0);
             }
-            slot ^= 1;
             lds_sync();
+        };
+        for (int st = s_begin; st < s_end; st += 2) {
+            stage(st, 1 % AD, 0);
+            if (st + 1 < s_end) stage(st + 1, 0, 1);
         }
     }
 

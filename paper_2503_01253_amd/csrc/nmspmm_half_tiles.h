@@ -8,21 +8,21 @@ namespace nmspmm {
 
 struct HalfTileArgs;
 
-// X(MI, CT, NG, RT, WR, WC, WK, NB, LDS KB, loads that need no alignment too)
+// X(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS KB, loads that need no alignment too)
 #define NMSPMM_HALF_TILES(X)                              \
-    X(32, 1, 2, 4, 1, 4, 1, 2, 80, 0) /* 128 x 256 */     \
-    X(32, 1, 1, 4, 1, 4, 1, 2, 80, 0) /* 128 x 128 */     \
-    X(32, 1, 1, 2, 1, 4, 2, 1, 80, 1) /* 64 x 128 */      \
-    X(32, 1, 1, 2, 1, 2, 4, 1, 80, 0) /* 64 x 64 */       \
-    X(32, 1, 1, 1, 1, 2, 4, 1, 80, 0) /* 32 x 64 */       \
-    X(32, 1, 1, 1, 1, 1, 8, 1, 80, 0) /* 32 x 32 */       \
-    X(32, 2, 1, 4, 1, 4, 1, 2, 80, 0) /* 128 x 256 */     \
-    X(32, 2, 1, 2, 2, 2, 1, 2, 80, 0) /* 128 x 128 */     \
-    X(32, 2, 1, 2, 1, 2, 2, 2, 80, 0) /* 64 x 128 */      \
-    X(32, 2, 1, 1, 1, 1, 8, 1, 80, 0) /* 32 x 64 */       \
-    X(16, 1, 2, 8, 1, 4, 1, 2, 80, 1) /* 128 x 128 */     \
-    X(16, 1, 2, 4, 1, 2, 4, 1, 80, 0) /* 64 x 64 */       \
-    X(16, 1, 2, 2, 1, 1, 8, 1, 80, 0) /* 32 x 32 */
+    X(32, 1, 2, 4, 1, 4, 1, 2, 1, 80, 0) /* 128 x 256 */     \
+    X(32, 1, 1, 4, 1, 4, 1, 2, 2, 80, 0) /* 128 x 128 */     \
+    X(32, 1, 1, 2, 1, 4, 2, 1, 2, 80, 1) /* 64 x 128 */      \
+    X(32, 1, 1, 2, 1, 2, 4, 1, 2, 80, 0) /* 64 x 64 */       \
+    X(32, 1, 1, 1, 1, 2, 4, 1, 2, 80, 0) /* 32 x 64 */       \
+    X(32, 1, 1, 1, 1, 1, 8, 1, 2, 80, 0) /* 32 x 32 */       \
+    X(32, 2, 1, 4, 1, 4, 1, 2, 1, 80, 0) /* 128 x 256 */     \
+    X(32, 2, 1, 2, 2, 2, 1, 2, 2, 80, 0) /* 128 x 128 */     \
+    X(32, 2, 1, 2, 1, 2, 2, 2, 2, 80, 0) /* 64 x 128 */      \
+    X(32, 2, 1, 1, 1, 1, 8, 1, 2, 80, 0) /* 32 x 64 */       \
+    X(16, 1, 2, 8, 1, 4, 1, 2, 1, 80, 1) /* 128 x 128 */     \
+    X(16, 1, 2, 4, 1, 2, 4, 1, 1, 80, 0) /* 64 x 64 */       \
+    X(16, 1, 2, 2, 1, 1, 8, 1, 2, 80, 0) /* 32 x 32 */
 
 // A stage of 1 to 4 operands a wave.
 constexpr int HALF_MAX_QS = 4;
