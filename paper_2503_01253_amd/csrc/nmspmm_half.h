@@ -65,9 +65,15 @@ __device__ __forceinline__ void half_store8(const HalfEpilogue &e, int64_t i, in
 #pragma unroll
         for (int x = 0; x < 8; ++x) y[x] += z[x];
     }
-    if (e.act != NMSPMM_HALF_ACT_NONE) {
+    if (e.act == NMSPMM_HALF_ACT_RELU) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x) y[x] = half_act(y[x], e.act);
+        for (int x = 0; x < 8; ++x) y[x] = half_act(y[x], NMSPMM_HALF_ACT_RELU);
+    } else if (e.act == NMSPMM_HALF_ACT_GELU) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) y[x] = half_act(y[x], NMSPMM_HALF_ACT_GELU);
+    } else if (e.act == NMSPMM_HALF_ACT_SILU) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) y[x] = half_act(y[x], NMSPMM_HALF_ACT_SILU);
     }
     if (e.mul) {
         load_row<8, true>(static_cast<const O *>(e.mul) + i * e.ld_mul + j, 8, z);

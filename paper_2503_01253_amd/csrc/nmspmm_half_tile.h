@@ -339,7 +339,10 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
     constexpr int CW = C::CW, CP = C::CPITCH, LPR = CW / 8, RPP = 64 / LPR;
     float *turn = reinterpret_cast<float *>(lds) + wave * (MI * CP);
     const int64_t j = col0 + wc * CW + lane % LPR * 8;
-#pragma unroll
+    // One copy of the code: unrolled over the row tiles it was larger than the
+    // instruction cache, and fetching it cost 40 us at 4096^3.  The row tiles
+    // move down through the first one's registers.
+#pragma unroll 1
     for (int t = 0; t < RT; ++t) {
 #pragma unroll
         for (int g = 0; g < NG; ++g)
@@ -348,28 +351,27 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const int r = MI == 32 ? 8 * (e / 4) + 4 * (lane / 32) + e % 4 : 4 * (lane / 16) + e;
-                    turn[r * CP + (g * CT + c) * MI + lane % MI] = acc[g][t][c][e];
+                    turn[r * CP + (g * CT + c) * MI + lane % MI] = acc[g][0][c][e];
                 }
         asm volatile("" ::: "memory");
-#pragma unroll
-        for (int r = 0; r < MI; r += RPP) {
-            const int row = r + lane / LPR;
-            const int64_t i = row0 + (wr * RT + t) * MI + row;
+#pragma unroll 1
+        for (int r = lane / LPR; r < MI; r += RPP) {
+            const int64_t i = row0 + (wr * RT + t) * MI + r;
             float x[8];
-            const f32x4 lo = *reinterpret_cast<const f32x4 *>(turn + row * CP + lane % LPR * 8);
-            const f32x4 hi = *reinterpret_cast<const f32x4 *>(turn + row * CP + lane % LPR * 8 + 4);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                x[y] = lo[y];
-                x[4 + y] = hi[y];
-            }
-            if (row < MI && i < p.m && j < p.n) {
+            load_row<8, true>(turn + r * CP + lane % LPR * 8, 8, x);
+            if (i < p.m && j < p.n) {
                 if (p.splits > 1) store_row<8, true>(p.part + ((int64_t)split * p.m + i) * p.n + j, 8, x);
                 else if (p.epi.f32) half_store8<float>(p.epi, i, j, x);
                 else half_store8<T>(p.epi, i, j, x);
             }
         }
         asm volatile("" ::: "memory");
+#pragma unroll
+        for (int u = 0; u + 1 < RT; ++u)
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) acc[g][u][c] = acc[g][u + 1][c];
     }
 }
 
