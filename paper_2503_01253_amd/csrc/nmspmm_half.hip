@@ -3,10 +3,12 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <cstdio>
 
 #include "nmspmm_half.h"
+#include "nmspmm_half_short.h"
 #include "nmspmm_half_tile.h"
 #include "nmspmm_half_tiles.h"
 #include "nmspmm_internal.h"
@@ -200,17 +202,22 @@ hipError_t launch_general(const GeneralArgs &p, hipStream_t stream)
 
 // ---- the tiled kernel ------------------------------------------------------
 
-// The split parts of C added in order, then the epilogue.
+// The split parts of C added in order, then the epilogue, eight columns a
+// thread (n is a multiple of 16 here).
 template <class O>
 __global__ __launch_bounds__(256) void nm_half_join_kernel(const float *part, int64_t m, int64_t n, int splits,
                                                            HalfEpilogue epi)
 {
-    const int64_t stride = (int64_t)gridDim.x * 256;
-    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < m * n; e += stride) {
-        float sum = 0.f;
-        for (int s = 0; s < splits; ++s) sum += part[s * m * n + e];
-        half_store<O>(epi, e / n, e % n, sum);
+    const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (e >= m * n) return;
+    float sum[8] = {}, x[8];
+    for (int s = 0; s < splits; ++s) {
+        load_row<8, true>(part + s * m * n + e, 8, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += x[i];
     }
+    const int64_t row = e / n;
+    half_store8<O>(epi, row, e - row * n, sum);
 }
 
 struct HalfTileInfo {
@@ -227,23 +234,33 @@ const HalfTileInfo half_tiles[] = {NMSPMM_HALF_TILES(NMSPMM_HALF_INFO)};
 #undef NMSPMM_HALF_INFO
 constexpr int half_tile_count = sizeof half_tiles / sizeof half_tiles[0];
 
+constexpr int HALF_SHORT = 1000;
+
 struct HalfPlan {
-    int tile = -1;      // none: the general kernel
+    int tile = -1;      // the tiled kernel's shape, HALF_SHORT, or none: the general kernel
     int QS = 0, P = 0, nst = 0, tiles_m = 0, tiles_n = 0, splits = 1;
+    int chunk_units = 0, chunks = 0;    // of HALF_SHORT
+    bool wide = false;
     bool vec = true;
     int64_t ws_bytes = 0;
 };
 
-// An estimate of a tile's time, in cycles of a CU: rounds of tiles times the
-// larger of a tile's matrix work, its LDS traffic and what it loads from L2.
-double half_cost(const HalfTileInfo &t, const HalfLayout &l, int64_t tiles)
+// An estimate of the tiled kernel's time in us.  A CU's W workgroups run two
+// at a time, each through its stages; a stage takes 0.8 us at least (its
+// barrier, the latencies of its loads and reads), and where the CU is full
+// what it loads from L2 (134 bytes a ns), writes into LDS (100, 32-row tiles
+// half that) and multiplies (6.45 GFLOP/s a CU) take their time one after
+// another.  (Fitted on MI355X: 4096^3 at 16:32 and V = 64 128 x 256 tiles 89 us
+// measured, 96 estimated; 128 x 128 118 and 131; 37 x 4096 x 11008 at 8:32 64 x 64 tiles 15.6 and
+// 15.8, 64 x 128 17.3 and 16.4; 128 x 4096 x 4096 at 16:32 32 x 64 13.0 and
+// 11.7, 64 x 64 17.6 and 16.4.)
+double half_cost(const HalfTileInfo &t, const HalfLayout &l, int P, int QS, int64_t workgroups, int stages)
 {
-    const double rounds = (double)((tiles + 511) / 512) * 2;
-    const double slots = (double)l.units * l.S * l.STEP, cols = (double)l.units * l.KR;
-    const double mfma = 2.0 * t.BM * t.BN * slots / 4096;
-    const double lds = (slots * t.BM * 2 * (t.BN / (t.CT * t.MI)) + cols * t.BM * 2) / 100;
-    const double l2 = (cols * t.BM * 2 + slots * t.BN * 2) / 40;
-    return rounds * (std::max({mfma, lds, l2}) + 2000);
+    const double a = 2.0 * t.BM * P * l.KR, slots = (double)QS * t.WK * l.STEP;
+    const double full = (a / 134 + a / (t.BM == 32 ? 50 : 100) + 2.0 * t.BN * slots / 134) * 1e-3 +
+                        2.0 * t.BM * t.BN * slots / 6.45e6;
+    const double W = (double)((workgroups + 255) / 256);
+    return 3 + stages * std::max(0.8 * std::ceil(W / 2), W * full);
 }
 
 // vec: A's rows start on 16 bytes.
@@ -252,6 +269,20 @@ HalfPlan half_plan(int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w
     HalfPlan best;
     if (l.MI == 0 || w.k == 0 || w.k >= (int64_t)1 << 21) return best;
     double best_cost = 1e300;
+    if (m <= HS_ROWS && vec && l.S * l.STEP == l.G * w.N && l.windows % l.G == 0) {
+        // the largest chunk of A that a slot holds, then the chunks made even
+        best.wide = w.n / l.MI <= 256;
+        const int slot = best.wide ? HS_SLOT_WIDE : HS_SLOT;
+        int64_t units = round_up(l.units, HS_NW);
+        while (units > 0 && m * half_short_pitch((int)std::min<int64_t>(units, 1 << 16), l.KR) > slot) units -= HS_NW;
+        if (units > 0) {
+            best.tile = HALF_SHORT;
+            best.chunks = (int)((l.units + units - 1) / units);
+            best.chunk_units = (int)round_up((l.units + best.chunks - 1) / best.chunks, HS_NW);
+            best.chunks = (int)((l.units + best.chunk_units - 1) / best.chunk_units);
+            best_cost = 0;
+        }
+    }
     for (int i = 0; i < half_tile_count; ++i) {
         const HalfTileInfo &t = half_tiles[i];
         if (t.MI != l.MI) continue;
@@ -270,13 +301,19 @@ HalfPlan half_plan(int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w
         c.nst = (int)((l.units + c.P - 1) / c.P);
         c.tiles_m = (int)tiles_m;
         c.tiles_n = (int)tiles_n;
-        const double cost = half_cost(t, l, tiles_m * tiles_n);
-        if (cost < best_cost) {
-            best_cost = cost;
-            best = c;
+        // k in several slices where the tiles leave CUs idle; joining them costs
+        // a launch and the parts' way through memory
+        const int most = may_split && tiles_m * tiles_n < 256 ? std::min(c.nst, 16) : 1;
+        for (c.splits = 1; c.splits <= most; ++c.splits) {
+            c.ws_bytes = c.splits > 1 ? c.splits * m * w.n * 4 : 0;
+            double cost = half_cost(t, l, c.P, c.QS, tiles_m * tiles_n * c.splits, (c.nst + c.splits - 1) / c.splits);
+            if (c.splits > 1) cost += 3 + (c.splits + 1) * m * w.n * 4 / 2e6;
+            if (cost < best_cost) {
+                best_cost = cost;
+                best = c;
+            }
         }
     }
-    (void)may_split;
     return best;
 }
 
@@ -342,6 +379,24 @@ hipError_t run(const HalfPlan &c, const HalfLayout &l, const void *A, int64_t ld
         p.epi = epi;
         return launch_general<T>(p, stream);
     }
+    if (c.tile == HALF_SHORT) {
+        HalfShortArgs p{};
+        p.A = A;
+        p.vals = reinterpret_cast<const unsigned char *>(base);
+        p.offs = reinterpret_cast<const uint16_t *>(base + l.offs_at);
+        p.lda = lda;
+        p.n = w.n;
+        p.k = w.k;
+        p.m = (int)m;
+        p.V = w.V;
+        p.S = l.S;
+        p.KR = l.KR;
+        p.steps = (int)l.steps;
+        p.chunk_units = c.chunk_units;
+        p.chunks = c.chunks;
+        p.epi = epi;
+        return launch_half_short(l.MI, p, w.dtype == NMSPMM_BF16, c.wide, stream);
+    }
     HalfTileArgs p{};
     p.A = A;
     p.vals = reinterpret_cast<const unsigned char *>(base);
@@ -367,7 +422,7 @@ hipError_t run(const HalfPlan &c, const HalfLayout &l, const void *A, int64_t ld
                  : c.QS == 3 ? launch_half_q3(c.tile, p, bf16, c.vec, stream)
                              : launch_half_q4(c.tile, p, bf16, c.vec, stream);
     if (e == hipSuccess && c.splits > 1) {
-        const unsigned blocks = (unsigned)std::min<int64_t>(8192, (m * w.n + 255) / 256);
+        const unsigned blocks = (unsigned)((m * w.n + 2047) / 2048);
         if (epi.f32)
             hipLaunchKernelGGL((nm_half_join_kernel<float>), dim3(blocks), dim3(256), 0, stream, p.part, m, w.n, c.splits, epi);
         else
@@ -428,6 +483,10 @@ extern "C" const char *nmspmm_half_kernel_name(int64_t m, const nmspmm_half_weig
     const HalfPlan c = half_plan(m, l, *weight, true, with_workspace != 0);
     if (c.tile < 0) return "nm_half_general_kernel";
     thread_local char buf[128];
+    if (c.tile == HALF_SHORT) {
+        std::snprintf(buf, sizeof buf, "nm_half_short_kernel<mi%d>,chunks%d", l.MI, c.chunks);
+        return buf;
+    }
     const HalfTileInfo &t = half_tiles[c.tile];
     std::snprintf(buf, sizeof buf, "nm_half_tile_kernel<%dx%d,mi%d,wk%d,qs%d>,stage%d,split%d", t.BM, t.BN, t.MI,
                   t.WK, c.QS, c.P * l.KR, c.splits);

@@ -7,6 +7,7 @@
 namespace nmspmm {
 
 struct HalfTileArgs;
+struct HalfShortArgs;
 
 // X(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS KB, loads that need no alignment too)
 #define NMSPMM_HALF_TILES(X)                              \
@@ -32,6 +33,9 @@ hipError_t launch_half_q1(int tile, const HalfTileArgs &a, bool bf16, bool vec, 
 hipError_t launch_half_q2(int tile, const HalfTileArgs &a, bool bf16, bool vec, hipStream_t stream);
 hipError_t launch_half_q3(int tile, const HalfTileArgs &a, bool bf16, bool vec, hipStream_t stream);
 hipError_t launch_half_q4(int tile, const HalfTileArgs &a, bool bf16, bool vec, hipStream_t stream);
+
+// Launches the kernel of few rows (nmspmm_half_short.h), with its wide slots or the others.
+hipError_t launch_half_short(int MI, const HalfShortArgs &a, bool bf16, bool wide, hipStream_t stream);
 
 }  // namespace nmspmm
 
