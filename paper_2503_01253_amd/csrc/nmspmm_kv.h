@@ -119,6 +119,11 @@ __device__ __forceinline__ void attend_store(const AttendArgs &p, const AttendTa
     }
 }
 
+// nmspmm_kv_mfma.hip: queries and cache of one 16-bit type, rows of whole
+// 16-byte pieces, at most 256 dimensions; tiles of 16 heads.
+constexpr int ATTEND_MFMA_HEADS = 16;
+void launch_attend_mfma(const AttendArgs &p, unsigned groups, hipStream_t stream);
+
 }  // namespace nmspmm
 
 #endif

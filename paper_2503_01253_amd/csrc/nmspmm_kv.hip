@@ -312,20 +312,20 @@ struct AttendPlan {
     int64_t ml_bytes, bytes;    // workspace
 };
 
-AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window, bool split)
+AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window, bool mfma,
+                       bool split)
 {
     AttendPlan a{};
     const int64_t group = q_heads / c->heads;
-    a.GT = group >= 5 ? 8 : group >= 3 ? 4 : (int)group;
+    a.GT = mfma ? ATTEND_MFMA_HEADS : group >= 5 ? 8 : group >= 3 ? 4 : (int)group;
     a.gtiles = (int)((group + a.GT - 1) / a.GT);
     int64_t span = std::min(max_length, table_positions(c));
     if (window > 0) span = std::min(span, window);
     const int64_t base = c->sequences * c->heads * a.gtiles;
-    // four workgroups a CU, each of 256 positions at least
+    // 12 workgroups a CU (three run at once), each of 256 positions at least
     int64_t splits = 1;
-    if (split && base > 0) splits = std::max<int64_t>(1, std::min<int64_t>((1024 + base - 1) / base, span / 256));
-    a.chunk = (int)std::max<int64_t>(64, (span + splits - 1) / splits);
-    a.chunk = (int)std::min<int64_t>(INT31 - 63, (a.chunk + 63) / 64 * 64);
+    if (split && base > 0) splits = std::max<int64_t>(1, std::min<int64_t>((3072 + base - 1) / base, span / 256));
+    a.chunk = (int)std::min<int64_t>(INT31 - 127, std::max<int64_t>(128, ((span + splits - 1) / splits + 127) / 128 * 128));
     a.splits = (int)std::max<int64_t>(1, (span + a.chunk - 1) / a.chunk);
     a.groups = base * a.splits;
     a.rows = c->sequences * q_heads;
@@ -334,6 +334,20 @@ AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_
         a.bytes = a.ml_bytes + a.rows * a.splits * c->dim * 4;
     }
     return a;
+}
+
+// Whether the matrix-core kernel takes the call: one 16-bit type, rows of
+// whole 16-byte pieces, and a cache whose pieces are counted in 32 bits.
+bool attend_takes_mfma(const nmspmm_kv_cache_t *c, nmspmm_dtype_t dtype)
+{
+    if (dtype == NMSPMM_F32 || dtype != c->dtype || c->dim > 256) return false;
+    for (const int64_t *stride : {c->k_stride, c->v_stride}) {
+        const int64_t limit = (int64_t)1 << 34;     // elements: 2^32 - 1 pieces hold every row's start
+        if (stride[0] < 0 || stride[1] < 0 || stride[0] > limit || stride[1] > limit) return false;
+        if (stride[0] && c->pages > limit / stride[0]) return false;
+        if (c->pages * stride[0] + c->page_size * stride[1] > limit) return false;
+    }
+    return rows_aligned(c->k_pages, c->k_stride, 3, c->dim, 2) && rows_aligned(c->v_pages, c->v_stride, 3, c->dim, 2);
 }
 
 template <class T, int LPT, int EPL, bool VEC>
@@ -437,7 +451,9 @@ extern "C" int64_t nmspmm_kv_attend_workspace_bytes(const nmspmm_kv_cache_t *cac
 {
     if (check_attend_sizes(cache, q_heads, max_length, window) != NMSPMM_OK) return -1;
     if (q_heads == 0 || cache->sequences == 0) return 0;
-    return attend_plan(cache, q_heads, max_length, window, true).bytes;
+    // of whichever kernel the types and strides will choose
+    return std::max(attend_plan(cache, q_heads, max_length, window, false, true).bytes,
+                    attend_plan(cache, q_heads, max_length, window, true, true).bytes);
 }
 
 extern "C" nmspmm_status_t nmspmm_kv_attend(const nmspmm_kv_cache_t *cache, const void *q, const int64_t *q_stride,
@@ -458,10 +474,11 @@ extern "C" nmspmm_status_t nmspmm_kv_attend(const nmspmm_kv_cache_t *cache, cons
         !aligned_to(workspace, 256))
         return NMSPMM_ERR_UNSUPPORTED;
     int cached = -1;
-    AttendPlan a = attend_plan(cache, q_heads, max_length, window, true);
+    const bool mfma = attend_takes_mfma(cache, dtype);
+    AttendPlan a = attend_plan(cache, q_heads, max_length, window, mfma, true);
     if (a.bytes > 0 && (!workspace || (uint64_t)a.bytes > (uint64_t)workspace_bytes)) {
         workspace = capturing(stream) ? nullptr : ws_acquire(stream, (size_t)a.bytes, &cached);
-        if (!workspace) a = attend_plan(cache, q_heads, max_length, window, false);
+        if (!workspace) a = attend_plan(cache, q_heads, max_length, window, mfma, false);
     }
     AttendArgs p{};
     p.c = device_view(cache);
@@ -490,7 +507,8 @@ extern "C" nmspmm_status_t nmspmm_kv_attend(const nmspmm_kv_cache_t *cache, cons
     const int cs = dtype_bytes(cache->dtype);
     const bool vec = rows_aligned(cache->k_pages, cache->k_stride, 3, cache->dim, cs) &&
                      rows_aligned(cache->v_pages, cache->v_stride, 3, cache->dim, cs);
-    if (cache->dtype == NMSPMM_F32) launch_attend<float>(p, vec, a.GT, (unsigned)a.groups, stream);
+    if (mfma) launch_attend_mfma(p, (unsigned)a.groups, stream);
+    else if (cache->dtype == NMSPMM_F32) launch_attend<float>(p, vec, a.GT, (unsigned)a.groups, stream);
     else if (cache->dtype == NMSPMM_BF16) launch_attend<bf16_t>(p, vec, a.GT, (unsigned)a.groups, stream);
     else launch_attend<f16_t>(p, vec, a.GT, (unsigned)a.groups, stream);
     hipError_t e = hipGetLastError();
