@@ -77,6 +77,19 @@ struct AppendArgs {
 
 constexpr int AP_NT = 256;
 
+// (a, b) turned by the angle of cos c and sin s.  Spelled with fused
+// multiply-adds whose fp32 results are kept (fp16's rounding is not fused into
+// them), so that every kernel rounds alike.
+__device__ __forceinline__ void turn_pair(float &a, float &b, float c, float s)
+{
+    float x = fmaf(a, c, -(b * s)), y = fmaf(a, s, b * c);
+#ifdef __HIP_DEVICE_COMPILE__
+    asm("" : "+v"(x), "+v"(y));
+#endif
+    a = x;
+    b = y;
+}
+
 // Every (token, row, dimension pair) by one thread: a row is a key, a value
 // or a query head; a pair is two dimensions that turn together, or (beyond
 // rot, and in values) two neighbours that are copied.  Elementwise, bound by
@@ -105,10 +118,7 @@ __global__ __launch_bounds__(AP_NT) void nm_append_kernel(AppendArgs p)
                         : static_cast<const T *>(p.q) + t * p.qn[0] + head * p.qn[1];
     float a = to_f32(src[d0]), b = d1 < p.dim ? to_f32(src[d1]) : 0.f;
     if (turn) {
-        const float c = p.cos[pos * half + e], s = p.sin[pos * half + e];
-        const float x = a * c - b * s;
-        b = a * s + b * c;
-        a = x;
+        turn_pair(a, b, p.cos[pos * half + e], p.sin[pos * half + e]);
     }
     if (is_k || is_v) {
         C *dst = is_k ? static_cast<C *>(p.k_pages) + at.page * p.c.ks[0] + at.slot * p.c.ks[1] + head * p.c.ks[2]
@@ -122,14 +132,79 @@ __global__ __launch_bounds__(AP_NT) void nm_append_kernel(AppendArgs p)
     }
 }
 
-template <class T>
-hipError_t launch_append(const AppendArgs &p, nmspmm_dtype_t cache, hipStream_t stream)
+constexpr int AV_NT = 128;
+
+// The same with eight pairs a thread, where every row holds whole 16-byte
+// pieces of eight dimensions and rot/2 is a multiple of 8: 16-byte accesses.
+// What does not depend on the position is asked for before anything is waited
+// for (64 tokens of 48 rows of 128: 11.4 us with one pair a thread and the
+// loads behind the checks).
+template <class T, class C>
+__global__ __launch_bounds__(AV_NT) void nm_append_vec_kernel(AppendArgs p)
 {
-    const dim3 grid((unsigned)p.tokens, (unsigned)((p.items + AP_NT - 1) / AP_NT));
-    if (cache == NMSPMM_F32) hipLaunchKernelGGL((nm_append_kernel<T, float>), grid, dim3(AP_NT), 0, stream, p);
-    else if (cache == NMSPMM_BF16) hipLaunchKernelGGL((nm_append_kernel<T, bf16_t>), grid, dim3(AP_NT), 0, stream, p);
-    else hipLaunchKernelGGL((nm_append_kernel<T, f16_t>), grid, dim3(AP_NT), 0, stream, p);
+    const int64_t t = blockIdx.x;
+    const int item = blockIdx.y * AV_NT + threadIdx.x;
+    if (item >= p.items) return;
+    const int64_t pos = p.pos[t], seq = p.seq[t];
+    const int pieces = p.dim / 16, row = item / pieces, e = item - row * pieces;
+    const bool is_k = row < p.heads, is_v = !is_k && row < 2 * p.heads;
+    const int head = is_k ? row : is_v ? row - p.heads : row - 2 * p.heads;
+    const int half = p.rot / 2;
+    const bool turn = !is_v && e * 8 < half, apart = turn && !p.interleaved;
+    const int d0 = apart ? e * 8 : e * 16, d1 = apart ? d0 + half : d0 + 8;
+    const T *src = is_k ? static_cast<const T *>(p.k_new) + t * p.kn[0] + head * p.kn[1]
+                 : is_v ? static_cast<const T *>(p.v_new) + t * p.vn[0] + head * p.vn[1]
+                        : static_cast<const T *>(p.q) + t * p.qn[0] + head * p.qn[1];
+    float a[8], b[8];
+    load_row<8, true>(src + d0, 8, a);
+    load_row<8, true>(src + d1, 8, b);
+    if (pos < 0 || pos >= p.table_positions || seq < 0 || seq >= p.sequences || (p.rot && pos >= p.positions)) return;
+    const Place at = place_of(p.c, p.c.table + seq * p.c.table_stride, (int)pos);
+    if (turn) {
+        float c[8], s[8];
+        load_row<8, true>(p.cos + pos * half + e * 8, 8, c);
+        load_row<8, true>(p.sin + pos * half + e * 8, 8, s);
+        if (apart) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) turn_pair(a[i], b[i], c[i], s[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                turn_pair(a[2 * i], a[2 * i + 1], c[i], s[i]);
+                turn_pair(b[2 * i], b[2 * i + 1], c[4 + i], s[4 + i]);
+            }
+        }
+    }
+    if (!at.held) return;
+    if (is_k || is_v) {
+        C *dst = is_k ? static_cast<C *>(p.k_pages) + at.page * p.c.ks[0] + at.slot * p.c.ks[1] + head * p.c.ks[2]
+                      : static_cast<C *>(p.v_pages) + at.page * p.c.vs[0] + at.slot * p.c.vs[1] + head * p.c.vs[2];
+        store_row<8, true>(dst + d0, 8, a);
+        store_row<8, true>(dst + d1, 8, b);
+    } else {
+        T *dst = static_cast<T *>(p.q_out) + t * p.qo[0] + head * p.qo[1];
+        store_row<8, true>(dst + d0, 8, a);
+        store_row<8, true>(dst + d1, 8, b);
+    }
+}
+
+template <class T, class C>
+hipError_t launch_append_to(AppendArgs p, bool vec, hipStream_t stream)
+{
+    const int rows = 2 * p.heads + p.q_heads;
+    p.items = rows * (vec ? p.dim / 16 : (p.dim + 1) / 2);
+    const int threads = vec ? AV_NT : AP_NT;
+    const dim3 grid((unsigned)p.tokens, (unsigned)((p.items + threads - 1) / threads));
+    if (vec) hipLaunchKernelGGL((nm_append_vec_kernel<T, C>), grid, dim3(AV_NT), 0, stream, p);
+    else hipLaunchKernelGGL((nm_append_kernel<T, C>), grid, dim3(AP_NT), 0, stream, p);
     return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch_append(const AppendArgs &p, nmspmm_dtype_t cache, bool vec, hipStream_t stream)
+{
+    if (cache == NMSPMM_F32) return launch_append_to<T, float>(p, vec, stream);
+    return cache == NMSPMM_BF16 ? launch_append_to<T, bf16_t>(p, vec, stream) : launch_append_to<T, f16_t>(p, vec, stream);
 }
 
 // ---- nmspmm_kv_attend ------------------------------------------------------
@@ -273,12 +348,16 @@ __global__ __launch_bounds__(AT_NT) void nm_attend_kernel(AttendArgs p)
     }
 }
 
-constexpr int JN_NT = 128;
+constexpr int JN_NT = 256, JN_GROUPS = JN_NT / 32, JN_D = KV_MAX_DIM;
 
-// The parts of a split sequence joined, one query head a workgroup, in the
-// order of the splits.
+// The parts of a split sequence joined, one query head a workgroup: eight
+// groups of 32 threads take the splits in turn, every 32nd dimension a thread, and
+// are added in their order.  (One thread a dimension over all splits, one
+// after another, took 180 us of 286 on one sequence of 131071 positions.)
 __global__ __launch_bounds__(JN_NT) void nm_attend_join_kernel(AttendArgs p)
 {
+    __shared__ float s_x[JN_GROUPS][JN_D];
+    __shared__ float s_sum[JN_GROUPS], s_top[JN_NT / 64];
     const int64_t row = blockIdx.x;
     const int64_t q_heads = (int64_t)p.heads * p.group;
     AttendTask t{};
@@ -286,20 +365,41 @@ __global__ __launch_bounds__(JN_NT) void nm_attend_join_kernel(AttendArgs p)
     const int64_t head = row % q_heads;
     const float2 *ml = p.part_ml + row * p.splits;
     float top = NEG_INF;
-    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, ml[s].x);
+    for (int s = threadIdx.x; s < p.splits; s += JN_NT) top = fmaxf(top, ml[s].x);
+#pragma unroll
+    for (int step = 32; step >= 1; step /= 2) top = fmaxf(top, __shfl_xor(top, step));
+    if (threadIdx.x % 64 == 0) s_top[threadIdx.x / 64] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < JN_NT / 64; ++w) top = fmaxf(top, s_top[w]);
     const float ref = softmax_ref(top);
+    const int group = threadIdx.x / 32, d0 = threadIdx.x % 32;
+    float x[JN_D / 32] = {}, sum = 0.f;
+    for (int s = group; s < p.splits; s += JN_GROUPS) {
+        const float2 e = ml[s];
+        if (e.x == NEG_INF && e.y == 0.f) continue;     // nothing there, and no sums written
+        const float c = exp2f(e.x - ref);
+        sum += c * e.y;
+        const float *part = p.part_acc + (row * p.splits + s) * p.dim;
+#pragma unroll
+        for (int i = 0; i < JN_D / 32; ++i)
+            if (i * 32 + d0 < p.dim) x[i] += c * part[i * 32 + d0];
+    }
+#pragma unroll
+    for (int i = 0; i < JN_D / 32; ++i)
+        if (i * 32 + d0 < p.dim) s_x[group][i * 32 + d0] = x[i];
+    if (d0 == 0) s_sum[group] = sum;
+    __syncthreads();
     AttendArgs whole = p;
     whole.splits = 1;
     for (int d = threadIdx.x; d < p.dim; d += JN_NT) {
-        float x = 0.f, sum = 0.f;
-        for (int s = 0; s < p.splits; ++s) {
-            const float2 e = ml[s];
-            if (e.x == NEG_INF && e.y == 0.f) continue;     // nothing there, and no sums written
-            const float c = exp2f(e.x - ref);
-            x += c * p.part_acc[(row * p.splits + s) * p.dim + d];
-            sum += c * e.y;
+        float y = 0.f, l = 0.f;
+#pragma unroll
+        for (int g = 0; g < JN_GROUPS; ++g) {
+            y += s_x[g][d];
+            l += s_sum[g];
         }
-        attend_store(whole, t, head, d, x, top, sum);
+        attend_store(whole, t, head, d, y, top, l);
     }
 }
 
@@ -322,9 +422,9 @@ AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_
     int64_t span = std::min(max_length, table_positions(c));
     if (window > 0) span = std::min(span, window);
     const int64_t base = c->sequences * c->heads * a.gtiles;
-    // 12 workgroups a CU (three run at once), each of 256 positions at least
+    // eight workgroups a CU (two or three run at once), each of 256 positions at least
     int64_t splits = 1;
-    if (split && base > 0) splits = std::max<int64_t>(1, std::min<int64_t>((3072 + base - 1) / base, span / 256));
+    if (split && base > 0) splits = std::max<int64_t>(1, std::min<int64_t>((2048 + base - 1) / base, span / 256));
     a.chunk = (int)std::min<int64_t>(INT31 - 127, std::max<int64_t>(128, ((span + splits - 1) / splits + 127) / 128 * 128));
     a.splits = (int)std::max<int64_t>(1, (span + a.chunk - 1) / a.chunk);
     a.groups = base * a.splits;
@@ -439,10 +539,16 @@ extern "C" nmspmm_status_t nmspmm_kv_append(const nmspmm_kv_cache_t *cache, cons
     p.dim = cache->dim;
     p.rot = rot;
     p.interleaved = interleaved != 0;
-    p.items = (int)items;
-    const hipError_t e = dtype == NMSPMM_F32 ? launch_append<float>(p, cache->dtype, stream)
-                       : dtype == NMSPMM_BF16 ? launch_append<bf16_t>(p, cache->dtype, stream)
-                                              : launch_append<f16_t>(p, cache->dtype, stream);
+    const int cs = dtype_bytes(cache->dtype);
+    const bool vec = cache->dim % 16 == 0 && rot % 16 == 0 && rows_aligned(k_new, k_stride, 2, cache->dim, es) &&
+                     rows_aligned(v_new, v_stride, 2, cache->dim, es) && aligned_to(cos, 16) && aligned_to(sin, 16) &&
+                     rows_aligned(cache->k_pages, cache->k_stride, 3, cache->dim, cs) &&
+                     rows_aligned(cache->v_pages, cache->v_stride, 3, cache->dim, cs) &&
+                     (q_heads == 0 || (rows_aligned(q, q_stride, 2, cache->dim, es) &&
+                                       rows_aligned(q_out, q_out_stride, 2, cache->dim, es)));
+    const hipError_t e = dtype == NMSPMM_F32 ? launch_append<float>(p, cache->dtype, vec, stream)
+                       : dtype == NMSPMM_BF16 ? launch_append<bf16_t>(p, cache->dtype, vec, stream)
+                                              : launch_append<f16_t>(p, cache->dtype, vec, stream);
     return e == hipSuccess ? NMSPMM_OK : NMSPMM_ERR_HIP;
 }
 

@@ -56,7 +56,7 @@ __device__ __forceinline__ float across_groups(float x, F f)
 
 // DK: pieces of 32 dimensions.
 template <class T, int DK>
-__global__ __launch_bounds__(AM_NT) void nm_attend_mfma_kernel(AttendArgs p)
+__global__ __launch_bounds__(AM_NT, DK <= 4 ? 3 : 2) void nm_attend_mfma_kernel(AttendArgs p)
 {
     constexpr int GT = 16, CPR = DK * 4, VL = CPR / 2, VPITCH = DK * 64 + 32, AP = DK * 32 + 4;
     static_assert(AM_NW * GT * AP * 4 <= AM_NW * AM_TOKENS * VPITCH, "the joining of the waves");
