@@ -348,16 +348,19 @@ __global__ __launch_bounds__(AT_NT) void nm_attend_kernel(AttendArgs p)
     }
 }
 
-constexpr int JN_NT = 256, JN_GROUPS = JN_NT / 32, JN_D = KV_MAX_DIM;
+constexpr int JN_NT = 512, JN_SPLITS = 2048, JN_U = 4;
 
-// The parts of a split sequence joined, one query head a workgroup: eight
-// groups of 32 threads take the splits in turn, every 32nd dimension a thread, and
-// are added in their order.  (One thread a dimension over all splits, one
-// after another, took 180 us of 286 on one sequence of 131071 positions.)
+// The parts of a split sequence joined, one query head a workgroup: the
+// weights of all splits first, then DL threads take a split's dimensions and
+// the workgroup's JN_NT / DL groups the splits in turn, JN_U of each asked for
+// at once; the groups are added in their order.  (One thread a dimension over
+// all splits, one after another, took 180 us of 286 on one sequence of 131071
+// positions; eight groups with one load at a time 52 of 176.)
+template <int DL, int DV>
 __global__ __launch_bounds__(JN_NT) void nm_attend_join_kernel(AttendArgs p)
 {
-    __shared__ float s_x[JN_GROUPS][JN_D];
-    __shared__ float s_sum[JN_GROUPS], s_top[JN_NT / 64];
+    constexpr int GROUPS = JN_NT / DL;
+    __shared__ float s_w[JN_SPLITS], s_x[GROUPS][DL * DV], s_top[JN_NT / 64], s_sum[JN_NT / 64];
     const int64_t row = blockIdx.x;
     const int64_t q_heads = (int64_t)p.heads * p.group;
     AttendTask t{};
@@ -373,34 +376,61 @@ __global__ __launch_bounds__(JN_NT) void nm_attend_join_kernel(AttendArgs p)
 #pragma unroll
     for (int w = 0; w < JN_NT / 64; ++w) top = fmaxf(top, s_top[w]);
     const float ref = softmax_ref(top);
-    const int group = threadIdx.x / 32, d0 = threadIdx.x % 32;
-    float x[JN_D / 32] = {}, sum = 0.f;
-    for (int s = group; s < p.splits; s += JN_GROUPS) {
+    float sum = 0.f;
+    for (int s = threadIdx.x; s < p.splits; s += JN_NT) {
         const float2 e = ml[s];
-        if (e.x == NEG_INF && e.y == 0.f) continue;     // nothing there, and no sums written
-        const float c = exp2f(e.x - ref);
+        // a split with nothing in it wrote no sums: its weight says so (negative)
+        const bool empty = e.x == NEG_INF && e.y == 0.f;
+        const float c = empty ? 0.f : exp2f(e.x - ref);
+        s_w[s] = empty ? -1.f : c;
         sum += c * e.y;
-        const float *part = p.part_acc + (row * p.splits + s) * p.dim;
-#pragma unroll
-        for (int i = 0; i < JN_D / 32; ++i)
-            if (i * 32 + d0 < p.dim) x[i] += c * part[i * 32 + d0];
     }
 #pragma unroll
-    for (int i = 0; i < JN_D / 32; ++i)
-        if (i * 32 + d0 < p.dim) s_x[group][i * 32 + d0] = x[i];
-    if (d0 == 0) s_sum[group] = sum;
+    for (int step = 32; step >= 1; step /= 2) sum += __shfl_xor(sum, step);
+    if (threadIdx.x % 64 == 0) s_sum[threadIdx.x / 64] = sum;
     __syncthreads();
+    const int group = threadIdx.x / DL, d = threadIdx.x % DL * DV;
+    float x[DV] = {};
+    if (d < p.dim)
+        for (int s = group; s < p.splits; s += GROUPS * JN_U) {
+            float v[JN_U][DV], w[JN_U];
+#pragma unroll
+            for (int u = 0; u < JN_U; ++u) {
+                const int at = s + u * GROUPS;
+                w[u] = at < p.splits ? s_w[at] : -1.f;
+                if (w[u] < 0.f) continue;
+#pragma unroll
+                for (int i = 0; i < DV; ++i) v[u][i] = p.part_acc[(row * p.splits + at) * p.dim + d + i];
+            }
+#pragma unroll
+            for (int u = 0; u < JN_U; ++u)
+#pragma unroll
+                for (int i = 0; i < DV; ++i) x[i] = w[u] < 0.f ? x[i] : fmaf(w[u], v[u][i], x[i]);
+        }
+#pragma unroll
+    for (int i = 0; i < DV; ++i) s_x[group][d + i] = x[i];
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < JN_NT / 64; ++w) sum += s_sum[w];
     AttendArgs whole = p;
     whole.splits = 1;
-    for (int d = threadIdx.x; d < p.dim; d += JN_NT) {
-        float y = 0.f, l = 0.f;
+    for (int i = threadIdx.x; i < p.dim; i += JN_NT) {
+        float y = 0.f;
 #pragma unroll
-        for (int g = 0; g < JN_GROUPS; ++g) {
-            y += s_x[g][d];
-            l += s_sum[g];
-        }
-        attend_store(whole, t, head, d, y, top, l);
+        for (int g = 0; g < GROUPS; ++g) y += s_x[g][i];
+        attend_store(whole, t, head, i, y, top, sum);
     }
+}
+
+// Four dimensions a thread where they come in fours.
+void launch_join(const AttendArgs &p, int64_t rows, hipStream_t stream)
+{
+    const dim3 grid((unsigned)rows), block(JN_NT);
+    if (p.dim % 4 == 0 && p.dim <= 64) hipLaunchKernelGGL((nm_attend_join_kernel<16, 4>), grid, block, 0, stream, p);
+    else if (p.dim % 4 == 0 && p.dim <= 128) hipLaunchKernelGGL((nm_attend_join_kernel<32, 4>), grid, block, 0, stream, p);
+    else if (p.dim % 4 == 0) hipLaunchKernelGGL((nm_attend_join_kernel<128, 4>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((nm_attend_join_kernel<512, 1>), grid, block, 0, stream, p);
 }
 
 // How the work is cut: query heads a workgroup takes together, workgroups
@@ -424,7 +454,7 @@ AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_
     const int64_t base = c->sequences * c->heads * a.gtiles;
     // eight workgroups a CU (two or three run at once), each of 256 positions at least
     int64_t splits = 1;
-    if (split && base > 0) splits = std::max<int64_t>(1, std::min<int64_t>((2048 + base - 1) / base, span / 256));
+    if (split && base > 0) splits = std::max<int64_t>(1, std::min<int64_t>((JN_SPLITS + base - 1) / base, span / 256));
     a.chunk = (int)std::min<int64_t>(INT31 - 127, std::max<int64_t>(128, ((span + splits - 1) / splits + 127) / 128 * 128));
     a.splits = (int)std::max<int64_t>(1, (span + a.chunk - 1) / a.chunk);
     a.groups = base * a.splits;
@@ -619,7 +649,7 @@ extern "C" nmspmm_status_t nmspmm_kv_attend(const nmspmm_kv_cache_t *cache, cons
     else launch_attend<f16_t>(p, vec, a.GT, (unsigned)a.groups, stream);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
-        hipLaunchKernelGGL(nm_attend_join_kernel, dim3((unsigned)a.rows), dim3(JN_NT), 0, stream, p);
+        launch_join(p, a.rows, stream);
         e = hipGetLastError();
     }
     const hipError_t f = cached >= 0 ? ws_done(cached, stream) : hipSuccess;

@@ -114,7 +114,7 @@ class HalfWeight:
         _library()
         if dtype not in _dtypes:
             raise TypeError(f"dtype must be torch.bfloat16 or torch.float16, not {dtype}")
-        self.packed, self.dtype, self.device = packed, dtype, packed.device
+        self.packed, self.dtype, self.device, self.at = packed, dtype, packed.device, packed.get_device()
         self.k, self.n, self.N, self.M, self.V = k, n, N, M, V
         self._c = _Weight(packed.data_ptr(), _dtypes[dtype], N, M, V, k, n)
         self._ref = ctypes.pointer(self._c)
@@ -180,32 +180,44 @@ def nmspmm_half_run(A, weight: HalfWeight, C, alpha: float = 1.0, bias=None, act
     nmspmm_half_workspace_bytes bytes (or None: the library's own)."""
     import torch
     L = _lib or _library()
-    dev = weight.device
-    _require("A", A, (weight.dtype,), 2, dev)
-    m = A.shape[0]
-    _shape("A", A, (m, weight.k))
-    _require("C", C, (weight.dtype, torch.float32), 2, dev)
-    _shape("C", C, (m, weight.n))
-    args = []
-    for name, t in (("mul", mul), ("residual", residual)):
-        if t is None:
-            args += [None, 0]
-        else:
-            _require(name, t, (C.dtype,), 2, dev)
-            _shape(name, t, C.shape)
-            args += [t.data_ptr(), t.stride(0)]
-    if bias is not None:
-        _require("bias", bias, (torch.float32,), 1, dev)
-        _shape("bias", bias, (weight.n,))
+    at = weight.at
+    dtype, c_dtype, shape, n = weight.dtype, C.dtype, C.shape, weight.n
+    extra = [x for x in (mul, residual) if x is not None]
+    # one expression for what holds in every good call (a call's host time is
+    # of the order of a small product's GPU time); _check_half words the rest
+    if not (A.dtype is dtype and (c_dtype is dtype or c_dtype is torch.float32) and A.get_device() == at
+            and C.get_device() == at and len(shape) == 2 and A.shape == (shape[0], weight.k) and shape[1] == n
+            and A.stride(1) == 1 and C.stride(1) == 1
+            and all(x.dtype is c_dtype and x.get_device() == at and x.shape == shape and x.stride(1) == 1 for x in extra)
+            and (bias is None or (bias.dtype is torch.float32 and bias.get_device() == at and bias.shape == (n,)
+                                  and bias.stride(0) == 1))):
+        _check_half(torch, A, weight, C, bias, mul, residual)
     if act not in HALF_ACTS:
         raise ValueError(f"act must be one of {sorted(HALF_ACTS)}")
-    at = C.get_device()
+    ws, size = (None, 0) if workspace is None else _workspace(workspace, weight.device)
     st = _call(torch, at, L.nmspmm_half_run, A.data_ptr(), A.stride(0), weight._ref, C.data_ptr(), C.stride(0),
-               _dtypes[C.dtype], m, alpha, None if bias is None else bias.data_ptr(), HALF_ACTS[act], *args,
-               *_workspace(workspace, dev), _raw_stream(torch, at, stream))
+               _dtypes[c_dtype], shape[0], alpha, None if bias is None else bias.data_ptr(), HALF_ACTS[act],
+               None if mul is None else mul.data_ptr(), 0 if mul is None else mul.stride(0),
+               None if residual is None else residual.data_ptr(), 0 if residual is None else residual.stride(0),
+               ws, size, _raw_stream(torch, at, stream))
     if st:
         _check("nmspmm_half_run", st)
     return C
+
+
+def _check_half(torch, A, weight, C, bias, mul, residual):
+    dev = weight.device
+    _require("A", A, (weight.dtype,), 2, dev)
+    _shape("A", A, (A.shape[0], weight.k))
+    _require("C", C, (weight.dtype, torch.float32), 2, dev)
+    _shape("C", C, (A.shape[0], weight.n))
+    for name, t in (("mul", mul), ("residual", residual)):
+        if t is not None:
+            _require(name, t, (C.dtype,), 2, dev)
+            _shape(name, t, C.shape)
+    if bias is not None:
+        _require("bias", bias, (torch.float32,), 1, dev)
+        _shape("bias", bias, (weight.n,))
 
 
 class KvCache:
@@ -223,7 +235,7 @@ class KvCache:
         _shape("v_pages", v_pages, k_pages.shape)
         _require("table", table, (torch.int32,), 2, k_pages.device)
         self.k_pages, self.v_pages, self.table = k_pages, v_pages, table
-        self.device, self.dtype = k_pages.device, k_pages.dtype
+        self.device, self.dtype, self.at = k_pages.device, k_pages.dtype, k_pages.get_device()
         self.pages, self.page_size, self.heads, self.dim = k_pages.shape
         self.sequences, self.table_pages = table.shape
         S = ctypes.c_int64 * 3
@@ -250,40 +262,63 @@ def nmspmm_kv_append(cache: KvCache, k, v, seq, pos, cos=None, sin=None, q=None,
     negative position, say) are skipped.  Returns q_out."""
     import torch
     L = _lib or _library()
-    dev = cache.device
-    _require("k", k, tuple(_dtypes), 3, dev)
-    kinds = (k.dtype,)
-    tokens = k.shape[0]
-    _shape("k", k, (tokens, cache.heads, cache.dim))
-    _require("v", v, kinds, 3, dev)
-    _shape("v", v, k.shape)
-    for name, t in (("seq", seq), ("pos", pos)):
-        _require(name, t, (torch.int32,), 1, dev)
-        _shape(name, t, (tokens,))
+    at, dtype, shape = cache.at, k.dtype, k.shape
+    if q is not None and q_out is None:
+        q_out = q
+    ks, vs = k.stride(), v.stride()
+    # as in nmspmm_half_run: one expression, and _check_append words the rest
+    if not (dtype in _dtypes and v.dtype is dtype and k.get_device() == at and v.get_device() == at
+            and len(shape) == 3 and v.shape == shape and shape[1] == cache.heads and shape[2] == cache.dim
+            and ks[2] == 1 and vs[2] == 1 and all(
+                x.dtype is torch.int32 and x.get_device() == at and x.shape == shape[:1] and x.stride(0) == 1
+                for x in (seq, pos))):
+        _check_append(torch, cache, k, v, seq, pos)
     angles = (None, None, 0, 0)
     if cos is not None or sin is not None:
-        for name, t in (("cos", cos), ("sin", sin)):
-            _require(name, t, (torch.float32,), 2, dev)
-            _shape(name, t, cos.shape)
-            if not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous")
-        angles = (cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1])
+        if not (cos.dtype is torch.float32 and sin.dtype is torch.float32 and cos.get_device() == at
+                and sin.get_device() == at and cos.dim() == 2 and sin.shape == cos.shape and cos.is_contiguous()
+                and sin.is_contiguous()):
+            _check_angles(torch, cache, cos, sin)
+        rows, half = cos.shape
+        angles = (cos.data_ptr(), sin.data_ptr(), rows, 2 * half)
     queries = (None, None, None, None, 0)
     if q is not None:
-        if q_out is None:
-            q_out = q
-        _require("q", q, kinds, 3, dev)
-        _shape("q", q, (tokens, q.shape[1], cache.dim))
-        _require("q_out", q_out, kinds, 3, dev)
-        _shape("q_out", q_out, q.shape)
-        queries = (q.data_ptr(), _Pair(*q.stride()[:2]), q_out.data_ptr(), _Pair(*q_out.stride()[:2]), q.shape[1])
-    at = k.get_device()
-    st = _call(torch, at, L.nmspmm_kv_append, cache._ref, k.data_ptr(), _Pair(*k.stride()[:2]), v.data_ptr(),
-               _Pair(*v.stride()[:2]), _dtypes[k.dtype], tokens, seq.data_ptr(), pos.data_ptr(), *angles,
-               int(interleaved), *queries, _raw_stream(torch, at, stream))
+        heads, qs, qos = q.shape[1], q.stride(), q_out.stride()
+        if not (q.dtype is dtype and q_out.dtype is dtype and q.get_device() == at and q_out.get_device() == at
+                and q.shape == (shape[0], heads, cache.dim) and q_out.shape == q.shape and qs[2] == 1 and qos[2] == 1):
+            _check_queries(cache, k, q, q_out)
+        queries = (q.data_ptr(), _Pair(qs[0], qs[1]), q_out.data_ptr(), _Pair(qos[0], qos[1]), heads)
+    st = _call(torch, at, L.nmspmm_kv_append, cache._ref, k.data_ptr(), _Pair(ks[0], ks[1]), v.data_ptr(),
+               _Pair(vs[0], vs[1]), _dtypes[dtype], shape[0], seq.data_ptr(), pos.data_ptr(), *angles,
+               interleaved, *queries, _raw_stream(torch, at, stream))
     if st:
         _check("nmspmm_kv_append", st)
     return q_out
+
+
+def _check_append(torch, cache, k, v, seq, pos):
+    _require("k", k, tuple(_dtypes), 3, cache.device)
+    _shape("k", k, (k.shape[0], cache.heads, cache.dim))
+    _require("v", v, (k.dtype,), 3, cache.device)
+    _shape("v", v, k.shape)
+    for name, t in (("seq", seq), ("pos", pos)):
+        _require(name, t, (torch.int32,), 1, cache.device)
+        _shape(name, t, k.shape[:1])
+
+
+def _check_angles(torch, cache, cos, sin):
+    for name, t in (("cos", cos), ("sin", sin)):
+        _require(name, t, (torch.float32,), 2, cache.device)
+        _shape(name, t, cos.shape)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+
+
+def _check_queries(cache, k, q, q_out):
+    _require("q", q, (k.dtype,), 3, cache.device)
+    _shape("q", q, (k.shape[0], q.shape[1], cache.dim))
+    _require("q_out", q_out, (k.dtype,), 3, cache.device)
+    _shape("q_out", q_out, q.shape)
 
 
 def nmspmm_kv_attend_workspace_bytes(cache: KvCache, q_heads: int, max_length: int, window: int = 0) -> int:
@@ -304,6 +339,27 @@ def nmspmm_kv_attend(cache: KvCache, q, lengths, out, scale=None, window: int = 
     bytes."""
     import torch
     L = _lib or _library()
+    at, dtype, shape, qs, outs = cache.at, q.dtype, q.shape, q.stride(), out.stride()
+    # as in nmspmm_half_run: one expression, and _check_attend words the rest
+    if not (dtype in _dtypes and out.dtype is dtype and q.get_device() == at and out.get_device() == at
+            and len(shape) == 3 and shape[0] == cache.sequences and shape[2] == cache.dim and out.shape == shape
+            and qs[2] == 1 and outs[2] == 1 and lengths.dtype is torch.int32 and lengths.get_device() == at
+            and lengths.shape == shape[:1] and lengths.stride(0) == 1 and lse is None):
+        _check_attend(torch, cache, q, lengths, out, lse)
+    if max_length is None:
+        max_length = cache.table_pages * cache.page_size
+    if scale is None:
+        scale = cache.dim ** -0.5
+    ws, size = (None, 0) if workspace is None else _workspace(workspace, cache.device)
+    st = _call(torch, at, L.nmspmm_kv_attend, cache._ref, q.data_ptr(), _Pair(qs[0], qs[1]), _dtypes[dtype],
+               shape[1], lengths.data_ptr(), max_length, window, scale, out.data_ptr(), _Pair(outs[0], outs[1]),
+               None if lse is None else lse.data_ptr(), ws, size, _raw_stream(torch, at, stream))
+    if st:
+        _check("nmspmm_kv_attend", st)
+    return out
+
+
+def _check_attend(torch, cache, q, lengths, out, lse):
     dev = cache.device
     _require("q", q, tuple(_dtypes), 3, dev)
     _shape("q", q, (cache.sequences, q.shape[1], cache.dim))
@@ -316,14 +372,3 @@ def nmspmm_kv_attend(cache: KvCache, q, lengths, out, scale=None, window: int = 
         _shape("lse", lse, q.shape[:2])
         if not lse.is_contiguous():
             raise ValueError("lse must be contiguous")
-    if max_length is None:
-        max_length = cache.table_pages * cache.page_size
-    if scale is None:
-        scale = cache.dim ** -0.5
-    at = q.get_device()
-    st = _call(torch, at, L.nmspmm_kv_attend, cache._ref, q.data_ptr(), _Pair(*q.stride()[:2]), _dtypes[q.dtype],
-               q.shape[1], lengths.data_ptr(), max_length, window, scale, out.data_ptr(), _Pair(*out.stride()[:2]),
-               None if lse is None else lse.data_ptr(), *_workspace(workspace, dev), _raw_stream(torch, at, stream))
-    if st:
-        _check("nmspmm_kv_attend", st)
-    return out
