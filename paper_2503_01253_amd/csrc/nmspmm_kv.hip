@@ -348,19 +348,19 @@ __global__ __launch_bounds__(AT_NT) void nm_attend_kernel(AttendArgs p)
     }
 }
 
-constexpr int JN_NT = 512, JN_SPLITS = 2048, JN_U = 4;
+constexpr int JN_SPLITS = 2048, JN_U = 4;
 
 // The parts of a split sequence joined, one query head a workgroup: the
 // weights of all splits first, then DL threads take a split's dimensions and
-// the workgroup's JN_NT / DL groups the splits in turn, JN_U of each asked for
+// the workgroup's NT / DL groups the splits in turn, JN_U of each asked for
 // at once; the groups are added in their order.  (One thread a dimension over
 // all splits, one after another, took 180 us of 286 on one sequence of 131071
 // positions; eight groups with one load at a time 52 of 176.)
-template <int DL, int DV>
-__global__ __launch_bounds__(JN_NT) void nm_attend_join_kernel(AttendArgs p)
+template <int NT, int SPLITS, int DL, int DV>
+__global__ __launch_bounds__(NT) void nm_attend_join_kernel(AttendArgs p)
 {
-    constexpr int GROUPS = JN_NT / DL;
-    __shared__ float s_w[JN_SPLITS], s_x[GROUPS][DL * DV], s_top[JN_NT / 64], s_sum[JN_NT / 64];
+    constexpr int GROUPS = NT / DL;
+    __shared__ float s_w[SPLITS], s_x[GROUPS][DL * DV], s_top[NT / 64], s_sum[NT / 64];
     const int64_t row = blockIdx.x;
     const int64_t q_heads = (int64_t)p.heads * p.group;
     AttendTask t{};
@@ -368,16 +368,16 @@ __global__ __launch_bounds__(JN_NT) void nm_attend_join_kernel(AttendArgs p)
     const int64_t head = row % q_heads;
     const float2 *ml = p.part_ml + row * p.splits;
     float top = NEG_INF;
-    for (int s = threadIdx.x; s < p.splits; s += JN_NT) top = fmaxf(top, ml[s].x);
+    for (int s = threadIdx.x; s < p.splits; s += NT) top = fmaxf(top, ml[s].x);
 #pragma unroll
     for (int step = 32; step >= 1; step /= 2) top = fmaxf(top, __shfl_xor(top, step));
     if (threadIdx.x % 64 == 0) s_top[threadIdx.x / 64] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < JN_NT / 64; ++w) top = fmaxf(top, s_top[w]);
+    for (int w = 0; w < NT / 64; ++w) top = fmaxf(top, s_top[w]);
     const float ref = softmax_ref(top);
     float sum = 0.f;
-    for (int s = threadIdx.x; s < p.splits; s += JN_NT) {
+    for (int s = threadIdx.x; s < p.splits; s += NT) {
         const float2 e = ml[s];
         // a split with nothing in it wrote no sums: its weight says so (negative)
         const bool empty = e.x == NEG_INF && e.y == 0.f;
@@ -412,10 +412,10 @@ __global__ __launch_bounds__(JN_NT) void nm_attend_join_kernel(AttendArgs p)
     __syncthreads();
     sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < JN_NT / 64; ++w) sum += s_sum[w];
+    for (int w = 0; w < NT / 64; ++w) sum += s_sum[w];
     AttendArgs whole = p;
     whole.splits = 1;
-    for (int i = threadIdx.x; i < p.dim; i += JN_NT) {
+    for (int i = threadIdx.x; i < p.dim; i += NT) {
         float y = 0.f;
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) y += s_x[g][i];
@@ -423,14 +423,25 @@ __global__ __launch_bounds__(JN_NT) void nm_attend_join_kernel(AttendArgs p)
     }
 }
 
+template <int DL, int DV>
+void launch_join_of(const AttendArgs &p, int64_t rows, hipStream_t stream)
+{
+    // few splits: small workgroups, of which a CU runs more (48 sequences x 64
+    // heads of 8 splits: 9.9 us with 512 threads)
+    constexpr int FEW = DL < 128 ? 128 : DL;
+    if (p.splits <= 16)
+        hipLaunchKernelGGL((nm_attend_join_kernel<FEW, 16, DL, DV>), dim3((unsigned)rows), dim3(FEW), 0, stream, p);
+    else
+        hipLaunchKernelGGL((nm_attend_join_kernel<512, JN_SPLITS, DL, DV>), dim3((unsigned)rows), dim3(512), 0, stream, p);
+}
+
 // Four dimensions a thread where they come in fours.
 void launch_join(const AttendArgs &p, int64_t rows, hipStream_t stream)
 {
-    const dim3 grid((unsigned)rows), block(JN_NT);
-    if (p.dim % 4 == 0 && p.dim <= 64) hipLaunchKernelGGL((nm_attend_join_kernel<16, 4>), grid, block, 0, stream, p);
-    else if (p.dim % 4 == 0 && p.dim <= 128) hipLaunchKernelGGL((nm_attend_join_kernel<32, 4>), grid, block, 0, stream, p);
-    else if (p.dim % 4 == 0) hipLaunchKernelGGL((nm_attend_join_kernel<128, 4>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((nm_attend_join_kernel<512, 1>), grid, block, 0, stream, p);
+    if (p.dim % 4 == 0 && p.dim <= 64) launch_join_of<16, 4>(p, rows, stream);
+    else if (p.dim % 4 == 0 && p.dim <= 128) launch_join_of<32, 4>(p, rows, stream);
+    else if (p.dim % 4 == 0) launch_join_of<128, 4>(p, rows, stream);
+    else launch_join_of<512, 1>(p, rows, stream);
 }
 
 // How the work is cut: query heads a workgroup takes together, workgroups
