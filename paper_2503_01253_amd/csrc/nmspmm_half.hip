@@ -29,7 +29,8 @@ int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 // in the same order, one per block and compressed row: the column c of the
 // unit as c * 8 + half_swz(c), or KR * 8 in padding rows; rows u and u + 4 of
 // each eight lie side by side, which is how a lane reads them, and a block's
-// end with a step of padding.  Other widths, and windows too long or of too
+// end with a step of padding.  The order of a unit's rows is the packing
+// kernel's.  Other widths, and windows too long or of too
 // many kept rows for a stage, keep Bc and idx as they are (MI = 0).
 struct HalfLayout {
     int MI, STEP, G, S, KR;
@@ -46,7 +47,8 @@ HalfLayout half_layout(int64_t k, int64_t n, int N, int M, int V)
     // the fewest windows whose rows fill their operands best: whole pieces of 8
     // columns, at most 128 (which bound the LDS a stage takes), and the operands
     // of a stage
-    const int MI = V % 16 ? 0 : V % 32 ? 16 : 32;
+    // (and a grid of units x blocks that the packing kernel can have)
+    const int MI = V % 16 || l.q > 65535 || l.windows >= (int64_t)1 << 24 ? 0 : V % 32 ? 16 : 32;
     double best = 0;
     for (int G = 1; MI && G * M <= 128; ++G) {
         const int step = 512 / MI, S = (G * N + step - 1) / step;
@@ -92,45 +94,77 @@ __global__ __launch_bounds__(256) void nm_half_pack_raw_kernel(const S *Bc, cons
     for (int64_t e = t; e < icount; e += stride) offs[e] = (uint8_t)(idx[e] < M ? idx[e] : M - 1);
 }
 
-// The compressed row in place `slot` of unit `unit`, or -1 for padding.
-__device__ __forceinline__ int64_t packed_row(const PackArgs &p, int64_t unit, int slot, int &window_of_unit)
-{
-    window_of_unit = slot / p.N;
-    const int64_t window = unit * p.l.G + window_of_unit;
-    return slot < p.l.G * p.N && window < p.l.windows ? window * p.N + slot % p.N : -1;
-}
-
+// One workgroup a unit of one column block.  The order of a unit's compressed
+// rows is free, as long as offsets and values agree: it is chosen so that the
+// LDS rows which one cycle of a transposed read touches (four of 64 bytes with
+// MI = 32, eight of 32 with MI = 16) lie on different banks where the unit's
+// columns allow.  Rows of one class of columns share their banks; the r-th row
+// of a class goes to group r, and what a class has beyond the number of groups
+// fills the places other classes leave, which are those of the last groups.
+// (In the order of the columns a read took 2.2 cycles more than it needs.)
 template <class T, class S>
-__global__ __launch_bounds__(256) void nm_half_pack_kernel(PackArgs p)
+__global__ __launch_bounds__(128) void nm_half_pack_kernel(PackArgs p)
 {
-    const int64_t stride = (int64_t)gridDim.x * 256, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int MI = p.l.MI, STEP = p.l.STEP;
-    const S *Bc = static_cast<const S *>(p.Bc);
-    T *vals = static_cast<T *>(p.vals);
-    const int64_t pieces = p.n / MI * p.l.steps * 64;       // of a lane's eight rows
-    for (int64_t e = t; e < pieces; e += stride) {
-        const int lane = (int)(e % 64);
-        const int64_t step = e / 64 % p.l.steps, tile = e / 64 / p.l.steps;
-        const int64_t col = tile * MI + lane % MI, unit = step / p.l.S;
-        const int first = (int)(step % p.l.S) * STEP + lane / MI * 8;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            int win;
-            const int64_t u = packed_row(p, unit, first + j, win);
-            vals[e * 8 + j] = u < 0 ? from_f32<T>(0.f) : from_f32<T>(to_f32(Bc[u * p.n + col]));
+    constexpr int SLOTS = HALF_MAX_QS * 32;
+    __shared__ int s_class[SLOTS], s_column[SLOTS], s_row[SLOTS];   // s_row: of a place, the row in it (-1: padding)
+    const int MI = p.l.MI, STEP = p.l.STEP, slots = p.l.S * STEP, rows = p.l.G * p.N;
+    const int64_t unit = blockIdx.x, block = blockIdx.y, first = unit * rows;
+    const int held = (int)(p.l.w - first < rows ? p.l.w - first : rows);
+    const int classes = MI == 32 ? 4 : 8, groups = slots / classes, i = threadIdx.x;
+    if (i < slots) {
+        s_row[i] = -1;
+        if (i < held) {
+            const int o = p.idx[(first + i) * p.l.q + block], c = i / p.N * p.M + (o < p.M ? o : p.M - 1);
+            s_column[i] = c;
+            s_class[i] = MI == 32 ? half_swz(c) >> 1 : half_swz(c);
         }
     }
-    const int64_t entries = p.l.q * (p.l.steps + 1) * STEP;
-    for (int64_t e = t; e < entries; e += stride) {
-        const int at = (int)(e % STEP);
-        const int64_t step = e / STEP % (p.l.steps + 1), block = e / STEP / (p.l.steps + 1), unit = step / p.l.S;
-        const int slot = (int)(step % p.l.S) * STEP + at / 8 * 8 + at % 8 / 2 + 4 * (at % 2);
-        int win;
-        const int64_t u = packed_row(p, unit, slot, win);
-        const int o = u < 0 ? 0 : p.idx[u * p.l.q + block];
-        const int c = win * p.M + (o < p.M ? o : p.M - 1);
-        p.offs[e] = u < 0 ? p.l.KR * 8 : c * 8 + half_swz(c);
+    __syncthreads();
+    // the place of class k's member of group g
+    auto place = [&](int g, int k) { return MI == 32 ? 4 * g + k : g / 2 * 16 + g % 2 * 4 + k % 4 + k / 4 * 8; };
+    if (i < held) {
+        int count[8] = {}, rank = 0;
+        for (int j = 0; j < held; ++j) {
+            const int k = s_class[j];
+            if (k == s_class[i] && j < i) ++rank;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) count[c] += c == k;
+        }
+        int spare = rank - groups;      // among the rows that find their class full
+        if (spare < 0) {
+            s_row[place(rank, s_class[i])] = i;
+        } else {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                if (c < s_class[i] && count[c] > groups) spare += count[c] - groups;
+            // the spare-th free place: from the last group down, as every class fills from the first
+            for (int g = groups - 1; g >= 0 && spare >= 0; --g)
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (c < classes && count[c] <= g && spare-- == 0) s_row[place(g, c)] = i;
+        }
     }
+    __syncthreads();
+    const S *Bc = static_cast<const S *>(p.Bc);
+    T *vals = static_cast<T *>(p.vals);
+    // a lane's eight rows, of every operand of the unit in the block's tiles
+    for (int e = i; e < p.V / MI * p.l.S * 64; e += 128) {
+        const int lane = e % 64, s = e / 64 % p.l.S;
+        const int64_t tile = block * (p.V / MI) + e / 64 / p.l.S, col = tile * MI + lane % MI;
+        T *dst = vals + ((tile * p.l.steps + unit * p.l.S + s) * 64 + lane) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int r = s_row[s * STEP + lane / MI * 8 + j];
+            dst[j] = r < 0 ? from_f32<T>(0.f) : from_f32<T>(to_f32(Bc[(first + r) * p.n + col]));
+        }
+    }
+    uint16_t *offs = p.offs + block * (p.l.steps + 1) * STEP;
+    const uint16_t padding = (uint16_t)(p.l.KR * 8);
+    for (int e = i; e < slots; e += 128) {
+        const int r = s_row[e / STEP * STEP + e % STEP / 8 * 8 + e % 8 / 2 + 4 * (e % 2)];
+        offs[unit * slots + e] = r < 0 ? padding : (uint16_t)(s_column[r] * 8 + half_swz(s_column[r]));
+    }
+    if (unit == p.l.units - 1 && i < STEP) offs[p.l.steps * STEP + i] = padding;     // the block's last step
 }
 
 // ---- any shape -------------------------------------------------------------
@@ -351,10 +385,11 @@ hipError_t pack(const void *Bc, nmspmm_dtype_t type, const uint8_t *idx, const n
         else
             hipLaunchKernelGGL((nm_half_pack_raw_kernel<T, T>), grid, dim3(256), 0, stream,
                                static_cast<const T *>(Bc), idx, vals, offs, count, icount, w.M);
-    } else if (type == NMSPMM_F32) {
-        hipLaunchKernelGGL((nm_half_pack_kernel<T, float>), grid, dim3(256), 0, stream, p);
     } else {
-        hipLaunchKernelGGL((nm_half_pack_kernel<T, T>), grid, dim3(256), 0, stream, p);
+        // (a layout with more blocks or units than a grid takes does not arise: see half_layout)
+        const dim3 units((unsigned)p.l.units, (unsigned)p.l.q);
+        if (type == NMSPMM_F32) hipLaunchKernelGGL((nm_half_pack_kernel<T, float>), units, dim3(128), 0, stream, p);
+        else hipLaunchKernelGGL((nm_half_pack_kernel<T, T>), units, dim3(128), 0, stream, p);
     }
     return hipGetLastError();
 }
