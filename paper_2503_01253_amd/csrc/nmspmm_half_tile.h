@@ -88,7 +88,7 @@ struct HalfTile {
     // waves a SIMD: two workgroups a CU where their LDS leaves room
     static constexpr int WPS = NT / 256 * (160 / LDS_KB_);
     static constexpr int RED_BYTES = WK > 1 ? (WK / 2) * WR * WC * ACCS * MI * MI * 4 : 0;
-    static constexpr int CW = CT * NG * MI, CPITCH = CW + 4;        // a wave's columns
+    static constexpr int CW = CT * NG * MI, CPITCH = CW + 8;        // a wave's columns, and rows 4 apart on other banks
     static_assert((RT & (RT - 1)) == 0 && PITCH == 2 * BM && RED_BYTES <= LDS_BYTES && WR * WC * WK * MI * CPITCH * 4 <= LDS_BYTES &&
                       64 / (CW / 8) <= MI, "tile shape");
     // rows of a slot, and columns of A of a stage, at most
@@ -142,12 +142,15 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
                                                     (uint32_t)(((rows_valid - 1) * p.lda + p.k) * 2));
     u32x4 ra[AD][NB][4];
     uint32_t a_off[NB], a_dst[NB];
-    // block b of this thread: rows 4*rb.., columns 8*kc.. of the stage (eight
-    // lanes to a row: whole 128-byte lines of A; halves of lines in different
-    // instructions waited for each other in L1)
+    // block b of this thread: rows 4*rb.., columns 8*kc.. of the stage.  A wave
+    // takes eight pieces of a row: whole 128-byte lines of A (halves of lines in
+    // different instructions waited for each other in L1); 16 of its lanes four
+    // pieces of four blocks of rows, which a cycle of a write finds on different
+    // banks (two of eight took twice the cycles).
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-        const int rb = ((tid + b * NT) >> 3) % (BM / 4), kc = (tid & 7) + 8 * ((tid + b * NT) / (2 * BM));
+        const int x = tid + b * NT, rb = ((x >> 2) & 3) + 4 * ((x >> 5) % (BM / 16));
+        const int kc = (x & 3) + 4 * ((x >> 4) & 1) + 8 * (x / (2 * BM));
         const int unit = 8 * kc / p.KR, c = 8 * kc - unit * p.KR;
         a_off[b] = 8 * kc < kstage ? (uint32_t)((4 * rb * p.lda + 8 * kc) * 2) : OOB;
         a_dst[b] = 8 * kc < kstage ? (uint32_t)((unit * (p.KR + 1) + c) * PITCH +
