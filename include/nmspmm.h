@@ -20,9 +20,9 @@
  * Every entry point is extern "C", returns a status code and never throws.
  * The library's only global state is the static scratch array of
  * nmspmm_run_noalloc (with its per-device address) and a table of at most 16
- * cached workspaces of nmspmm_run and nmspmm_run_ex, one per (device,
- * stream), allocated on first use and kept until the process ends; it is
- * safe to call from several host threads.
+ * cached workspaces of nmspmm_run, nmspmm_run_ex and the calls of
+ * nmspmm_serve.h, one per (device, stream), allocated on first use and kept
+ * until the process ends; it is safe to call from several host threads.
  */
 #ifndef NMSPMM_H
 #define NMSPMM_H

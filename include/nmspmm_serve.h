@@ -84,7 +84,7 @@ NMSPMM_API int64_t nmspmm_half_workspace_bytes(int64_t m, const nmspmm_half_weig
  *            it.  No other overlap of C with an input is allowed.
  * Products of two 16-bit values are exact in fp32; sums, epilogue and (where
  * k is split) partial sums are fp32; C is rounded once (ties to even).  The
- * order of summation is fixed by shape and workspace, so results do not vary
+ * order of summation is fixed by shape, alignment and workspace: results do not vary
  * between runs.  Only kept rows of B enter a sum: an infinity or NaN in a
  * column of A that a column block does not keep leaves that block alone.
  * m == 0 or n == 0 returns NMSPMM_OK without a launch; with k == 0 the sum is
@@ -140,8 +140,8 @@ typedef struct {
  * A value is rounded once to the cache's type (ties to even).  A token whose
  * sequence, position, page or (with cos) row of angles lies outside its array,
  * a negative position above all, is skipped: neither its keys and values nor
- * its q_out are written.  Two tokens of one call with one place leave one of
- * the two there.  tokens == 0 returns NMSPMM_OK without a launch.  Errors:
+ * its q_out are written.  Two tokens of one call with one place leave there, value
+ * by value, one of the two.  tokens == 0 returns NMSPMM_OK without a launch.  Errors:
  * NMSPMM_ERR_INVALID_ARG (negative size, bad type, odd rot or rot > dim, null
  * pointer with non-empty data), NMSPMM_ERR_UNSUPPORTED (misaligned pointer,
  * dim > 512, more than 2^31 - 1 tokens, heads or positions), NMSPMM_ERR_HIP. */
@@ -167,8 +167,8 @@ NMSPMM_API int64_t nmspmm_kv_attend_workspace_bytes(const nmspmm_kv_cache_t *cac
  *            are in the cache.  A length <= 0 leaves no position: that row of
  *            out is zero and its lse minus infinity.
  *   max_length  an upper bound of the lengths, known to the host, which sets
- *            how the work is split; a length beyond it or beyond the table is
- *            taken as the smaller of the two
+ *            how the work is split; a length beyond it, beyond the table or
+ *            beyond 2^31 - 4097 is taken as the smallest of these
  *   lse      sequences x q_heads fp32, the natural logarithm of the softmax's
  *            denominator (to join results over parts of a context), or NULL
  * A position whose page lies outside the cache is left out.  Positions outside
@@ -178,7 +178,8 @@ NMSPMM_API int64_t nmspmm_kv_attend_workspace_bytes(const nmspmm_kv_cache_t *cac
  * or no query heads: NMSPMM_OK without a launch.  Errors:
  * NMSPMM_ERR_INVALID_ARG (negative size, bad type, q_heads no multiple of
  * heads, null pointer with non-empty data), NMSPMM_ERR_UNSUPPORTED
- * (misaligned pointer, dim > 512, sizes beyond 2^31 - 1), NMSPMM_ERR_HIP. */
+ * (misaligned pointer, dim > 512, sizes beyond 2^31 - 1, 2^24 query rows or
+ * more), NMSPMM_ERR_HIP. */
 NMSPMM_API nmspmm_status_t nmspmm_kv_attend(const nmspmm_kv_cache_t *cache, const void *q, const int64_t *q_stride,
                                  nmspmm_dtype_t dtype, int64_t q_heads, const int32_t *lengths,
                                  int64_t max_length, int64_t window, float scale, void *out,

@@ -277,10 +277,22 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
 #pragma unroll
             for (int b = 0; b < NB; ++b) load_a(d % AD, b, s_begin + d);
         lds_sync();
+        // (debug build) NaN in the places that this thread's next stores will fill
+        auto poison_a = [&](int slot) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                if (a_dst[b] != OOB)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<u32x2 *>(lds + slot * slot_bytes + j * PITCH + (a_dst[b] ^ ((j & C::SWZ) << 5))) =
+                            u32x2{0x7fff7fffu, 0x7fff7fffu};
+            asm volatile("" ::: "memory");
+        };
         // the next stage's slab, which has been on its way for AD stages, is
         // written a part a step, and each block's registers take the one AD
         // stages on
         auto stage = [&](int st, int d, int slot) {
+            if constexpr (NMSPMM_POISON_LDS) poison_a(slot ^ 1);
 #pragma unroll
             for (int i = 0; i < QS; ++i) {
 #pragma unroll

@@ -641,7 +641,8 @@ extern "C" nmspmm_status_t nmspmm_kv_attend(const nmspmm_kv_cache_t *cache, cons
         p.qs[i] = q_stride[i];
         p.os[i] = out_stride[i];
     }
-    p.cap = (int)std::min(max_length, table_positions(cache));
+    // (the kernels step a few hundred positions past the last)
+    p.cap = (int)std::min({max_length, table_positions(cache), INT31 - 4096});
     p.window = (int)std::min(window, INT31);
     p.heads = cache->heads;
     p.group = (int)(q_heads / cache->heads);
