@@ -119,10 +119,10 @@ __device__ __forceinline__ void attend_store(const AttendArgs &p, const AttendTa
     }
 }
 
-// nmspmm_kv_mfma.hip: queries and cache of one 16-bit type, rows of whole
-// 16-byte pieces, at most 256 dimensions; tiles of 16 heads.
+// nmspmm_kv_mfma.hip: an fp16 cache with fp16 queries or a bf16 cache with any,
+// rows of whole 16-byte pieces, at most 256 dimensions; tiles of 16 heads.
 constexpr int ATTEND_MFMA_HEADS = 16;
-void launch_attend_mfma(const AttendArgs &p, unsigned groups, hipStream_t stream);
+void launch_attend_mfma(const AttendArgs &p, nmspmm_dtype_t cache, unsigned groups, hipStream_t stream);
 
 }  // namespace nmspmm
 

@@ -477,11 +477,12 @@ AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_
     return a;
 }
 
-// Whether the matrix-core kernel takes the call: one 16-bit type, rows of
+// Whether the matrix-core kernel takes the call: a bf16 cache, or fp16 queries
+// over an fp16 cache (whose range would not hold the parts of others), rows of
 // whole 16-byte pieces, and a cache whose pieces are counted in 32 bits.
 bool attend_takes_mfma(const nmspmm_kv_cache_t *c, nmspmm_dtype_t dtype)
 {
-    if (dtype == NMSPMM_F32 || dtype != c->dtype || c->dim > 256) return false;
+    if (c->dtype == NMSPMM_F32 || (c->dtype == NMSPMM_F16 && dtype != NMSPMM_F16) || c->dim > 256) return false;
     for (const int64_t *stride : {c->k_stride, c->v_stride}) {
         const int64_t limit = (int64_t)1 << 34;     // elements: 2^32 - 1 pieces hold every row's start
         if (stride[0] < 0 || stride[1] < 0 || stride[0] > limit || stride[1] > limit) return false;
@@ -655,7 +656,7 @@ extern "C" nmspmm_status_t nmspmm_kv_attend(const nmspmm_kv_cache_t *cache, cons
     const int cs = dtype_bytes(cache->dtype);
     const bool vec = rows_aligned(cache->k_pages, cache->k_stride, 3, cache->dim, cs) &&
                      rows_aligned(cache->v_pages, cache->v_stride, 3, cache->dim, cs);
-    if (mfma) launch_attend_mfma(p, (unsigned)a.groups, stream);
+    if (mfma) launch_attend_mfma(p, cache->dtype, (unsigned)a.groups, stream);
     else if (cache->dtype == NMSPMM_F32) launch_attend<float>(p, vec, a.GT, (unsigned)a.groups, stream);
     else if (cache->dtype == NMSPMM_BF16) launch_attend<bf16_t>(p, vec, a.GT, (unsigned)a.groups, stream);
     else launch_attend<f16_t>(p, vec, a.GT, (unsigned)a.groups, stream);

@@ -1,4 +1,5 @@
-// nmspmm_kv_attend on the matrix cores: queries and cache of one 16-bit type.
+// nmspmm_kv_attend on the matrix cores: queries and cache of one 16-bit type, or
+// queries of another type over a bf16 cache.
 //
 // A workgroup of four waves takes a tile of 16 query heads of one cache head
 // (fewer heads leave columns unused: the kernel is bound by the cache's bytes)
@@ -9,6 +10,10 @@
 //   P^T           running maximum of each head (a lane's column), weights in
 //                 fp32, each as two 16-bit parts (2^-17 of itself together;
 //                 one part alone would double the error of a 16-bit output);
+//                 queries that are not bf16 over a bf16 cache: three bf16 parts
+//                 of every query value and of every weight, which hold all 24
+//                 bits (a batch of 42 x 676 positions, 7 heads of 256, 87 us on
+//                 the vector ALU);
 //   O^T += V^T P^T  the weights lie in the lanes just as the B operand wants
 //                 them (k index 8g+j stands for token 4g+j, or 16+4g+j-4 from
 //                 j = 4 on); V goes through LDS, a wave's own piece, whose
@@ -41,6 +46,18 @@ __device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c)
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// x as PARTS 16-bit values, each the nearest to what those before it leave.
+template <class T, int PARTS>
+__device__ __forceinline__ void split_parts(float x, short (&part)[PARTS])
+{
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        const T h = from_f32<T>(x);
+        part[i] = __builtin_bit_cast(short, h);
+        x -= to_f32(h);
+    }
+}
+
 // The values of the lanes 16 and 32 away: after the swap one result holds the
 // even rows' value in both rows of a pair, the other the odd rows'.
 template <class F>
@@ -54,10 +71,11 @@ __device__ __forceinline__ float across_groups(float x, F f)
     return f(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
 }
 
-// DK: pieces of 32 dimensions.
-template <class T, int DK>
-__global__ __launch_bounds__(AM_NT, DK <= 4 ? 3 : 2) void nm_attend_mfma_kernel(AttendArgs p)
+// DK: pieces of 32 dimensions.  QP: parts of a query value.
+template <class T, int DK, int QP>
+__global__ __launch_bounds__(AM_NT, DK <= 4 && QP == 1 ? 3 : DK <= 4 ? 2 : 1) void nm_attend_mfma_kernel(AttendArgs p)
 {
+    constexpr int PP = QP == 1 ? 2 : 3;     // parts of a weight
     constexpr int GT = 16, CPR = DK * 4, VL = CPR / 2, VPITCH = DK * 64 + 32, AP = DK * 32 + 4;
     static_assert(AM_NW * GT * AP * 4 <= AM_NW * AM_TOKENS * VPITCH, "the joining of the waves");
     __shared__ __align__(16) unsigned char lds[AM_NW * AM_TOKENS * VPITCH];
@@ -73,14 +91,24 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 ? 3 : 2) void nm_attend_mfma_kernel(
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int col = lane & 15, grp = lane >> 4;
 
-    s16x8 q[DK];
+    s16x8 q[QP][DK];
 #pragma unroll
     for (int c = 0; c < DK; ++c)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int d = c * 32 + grp * 8 + j;
-            q[c][j] = col < t.heads_in_tile && d < p.dim
-                          ? static_cast<const short *>(p.q)[t.seq * p.qs[0] + (t.first_head + col) * p.qs[1] + d] : (short)0;
+            const bool there = col < t.heads_in_tile && d < p.dim;
+            const int64_t at = t.seq * p.qs[0] + (t.first_head + col) * p.qs[1] + d;
+            if constexpr (QP == 1) {
+                q[0][c][j] = there ? static_cast<const short *>(p.q)[at] : (short)0;
+            } else {
+                const float x = !there ? 0.f : p.io == NMSPMM_F32 ? static_cast<const float *>(p.q)[at]
+                                                                  : to_f32(static_cast<const f16_t *>(p.q)[at]);
+                short part[QP];
+                split_parts<T, QP>(x, part);
+#pragma unroll
+                for (int i = 0; i < QP; ++i) q[i][c][j] = part[i];
+            }
         }
 
     const int32_t *row = p.c.table + t.seq * p.c.table_stride;
@@ -138,8 +166,11 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 ? 3 : 2) void nm_attend_mfma_kernel(
         f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int c = 0; c < DK; ++c) {
-            s[0] = mfma16<T>(kr[0][c], q[c], s[0]);
-            s[1] = mfma16<T>(kr[1][c], q[c], s[1]);
+#pragma unroll
+            for (int i = QP - 1; i >= 0; --i) {     // the smallest parts first
+                s[0] = mfma16<T>(kr[0][c], q[i][c], s[0]);
+                s[1] = mfma16<T>(kr[1][c], q[i][c], s[1]);
+            }
         }
         load_k(next);
         float x[8];
@@ -162,14 +193,15 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 ? 3 : 2) void nm_attend_mfma_kernel(
             for (int b = 0; b < DK * 2; ++b) o[b] *= corr;
             m = top;
         }
-        s16x8 hi, lo;
+        s16x8 w[PP];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float w = __builtin_amdgcn_exp2f(x[j] - ref);
-            l += w;
-            const T h = from_f32<T>(w);
-            hi[j] = __builtin_bit_cast(short, h);
-            lo[j] = __builtin_bit_cast(short, from_f32<T>(w - to_f32(h)));
+            const float e = __builtin_amdgcn_exp2f(x[j] - ref);
+            l += e;
+            short part[PP];
+            split_parts<T, PP>(e, part);
+#pragma unroll
+            for (int i = 0; i < PP; ++i) w[i][j] = part[i];
         }
         asm volatile("" ::: "memory");
 #pragma unroll
@@ -188,8 +220,8 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 ? 3 : 2) void nm_attend_mfma_kernel(
             for (int y = 0; y < 2; ++y)
                 v[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(lds_u8 *)(uintptr_t)(vt + b * 32 + y * 16 * VPITCH));
             const s16x8 a = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
-            o[b] = mfma16<T>(a, hi, o[b]);
-            o[b] = mfma16<T>(a, lo, o[b]);
+#pragma unroll
+            for (int i = PP - 1; i >= 0; --i) o[b] = mfma16<T>(a, w[i], o[b]);
         }
     }
 
@@ -218,22 +250,23 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 ? 3 : 2) void nm_attend_mfma_kernel(
     }
 }
 
-template <class T>
+template <class T, int QP>
 void launch(const AttendArgs &p, unsigned groups, hipStream_t stream)
 {
     const dim3 grid(groups), block(AM_NT);
-    if (p.dim <= 64) hipLaunchKernelGGL((nm_attend_mfma_kernel<T, 2>), grid, block, 0, stream, p);
-    else if (p.dim <= 96) hipLaunchKernelGGL((nm_attend_mfma_kernel<T, 3>), grid, block, 0, stream, p);
-    else if (p.dim <= 128) hipLaunchKernelGGL((nm_attend_mfma_kernel<T, 4>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((nm_attend_mfma_kernel<T, 8>), grid, block, 0, stream, p);
+    if (p.dim <= 64) hipLaunchKernelGGL((nm_attend_mfma_kernel<T, 2, QP>), grid, block, 0, stream, p);
+    else if (p.dim <= 96) hipLaunchKernelGGL((nm_attend_mfma_kernel<T, 3, QP>), grid, block, 0, stream, p);
+    else if (p.dim <= 128) hipLaunchKernelGGL((nm_attend_mfma_kernel<T, 4, QP>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((nm_attend_mfma_kernel<T, 8, QP>), grid, block, 0, stream, p);
 }
 
 }  // namespace
 
-void launch_attend_mfma(const AttendArgs &p, unsigned groups, hipStream_t stream)
+void launch_attend_mfma(const AttendArgs &p, nmspmm_dtype_t cache, unsigned groups, hipStream_t stream)
 {
-    if (p.io == NMSPMM_BF16) launch<bf16_t>(p, groups, stream);
-    else launch<f16_t>(p, groups, stream);
+    if (cache == NMSPMM_F16) launch<f16_t, 1>(p, groups, stream);
+    else if (p.io == NMSPMM_BF16) launch<bf16_t, 1>(p, groups, stream);
+    else launch<bf16_t, 3>(p, groups, stream);
 }
 
 }  // namespace nmspmm
