@@ -43,9 +43,11 @@ __device__ __forceinline__ void half_store(const HalfEpilogue &e, int64_t i, int
     static_cast<O *>(e.C)[i * e.ldc + j] = from_f32<O>(y);
 }
 
-// Eight columns of row i from column j on, all inside C.
+// Eight columns of row i from column j on, all inside C.  `ahead`: where what
+// mul (or, without a mul, residual) holds there has been fetched to, or null.
 template <class O>
-__device__ __forceinline__ void half_store8(const HalfEpilogue &e, int64_t i, int64_t j, float (&y)[8])
+__device__ __forceinline__ void half_store8(const HalfEpilogue &e, int64_t i, int64_t j, float (&y)[8],
+                                            const O *ahead = nullptr)
 {
     float z[8];
     if (!e.vec) {
@@ -76,12 +78,12 @@ __device__ __forceinline__ void half_store8(const HalfEpilogue &e, int64_t i, in
         for (int x = 0; x < 8; ++x) y[x] = half_act(y[x], NMSPMM_HALF_ACT_SILU);
     }
     if (e.mul) {
-        load_row<8, true>(static_cast<const O *>(e.mul) + i * e.ld_mul + j, 8, z);
+        load_row<8, true>(ahead ? ahead : static_cast<const O *>(e.mul) + i * e.ld_mul + j, 8, z);
 #pragma unroll
         for (int x = 0; x < 8; ++x) y[x] *= z[x];
     }
     if (e.residual) {
-        load_row<8, true>(static_cast<const O *>(e.residual) + i * e.ld_residual + j, 8, z);
+        load_row<8, true>(ahead && !e.mul ? ahead : static_cast<const O *>(e.residual) + i * e.ld_residual + j, 8, z);
 #pragma unroll
         for (int x = 0; x < 8; ++x) y[x] += z[x];
     }

@@ -89,7 +89,7 @@ struct HalfTile {
     static constexpr int WPS = NT / 256 * (160 / LDS_KB_);
     static constexpr int RED_BYTES = WK > 1 ? (WK / 2) * WR * WC * ACCS * MI * MI * 4 : 0;
     static constexpr int CW = CT * NG * MI, CPITCH = CW + 8;        // a wave's columns, and rows 4 apart on other banks
-    static_assert((RT & (RT - 1)) == 0 && PITCH == 2 * BM && RED_BYTES <= LDS_BYTES && WR * WC * WK * MI * CPITCH * 4 <= LDS_BYTES &&
+    static_assert((RT & (RT - 1)) == 0 && PITCH == 2 * BM && RED_BYTES <= LDS_BYTES && WR * WC * (MI * CPITCH * 4 + 4 * MI * CW) <= LDS_BYTES &&
                       64 / (CW / 8) <= MI, "tile shape");
     // rows of a slot, and columns of A of a stage, at most
     static constexpr int ROWS = LDS_BYTES / 2 / PITCH, KMAX = NB * NT / (2 * BM) * 64;
@@ -354,11 +354,32 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
     constexpr int CW = C::CW, CP = C::CPITCH, LPR = CW / 8, RPP = 64 / LPR;
     float *turn = reinterpret_cast<float *>(lds) + wave * (MI * CP);
     const int64_t j = col0 + wc * CW + lane % LPR * 8;
+    // What the epilogue reads of mul (or residual) comes by DMA into LDS, the
+    // rows of two accumulators at once, each lane's pieces where it will look
+    // for them: loaded where they are used, eight waves a CU had too few bytes
+    // on their way (2048 x 4096 x 11008 at 8:32 with a factor 129 us, 125 so;
+    // 4096^3 at 16:32 with a term 108 and 103).
+    constexpr int PIECES = MI / RPP, AHEAD = 2 * MI * CW * 2;      // a lane's of an accumulator; bytes of a wave
+    unsigned char *fetched = lds + WR * WC * (MI * CP * 4) + wave * AHEAD;
+    const void *other = p.epi.mul ? p.epi.mul : p.epi.residual;
+    const int64_t ld_other = p.epi.mul ? p.epi.ld_mul : p.epi.ld_residual;
+    const bool fetch = other && p.epi.vec && !p.epi.f32 && p.splits == 1 && ld_other < (int64_t)1 << 21;
+    const __amdgpu_buffer_rsrc_t o_rsrc =
+        make_rsrc(static_cast<const T *>(other) + row0 * ld_other + col0,
+                  fetch ? (uint32_t)(((rows_valid - 1) * ld_other + min64(BN, p.n - col0)) * 2) : 0u);
     // One copy of the code: unrolled over the row tiles it was larger than the
     // instruction cache, and fetching it cost 40 us at 4096^3.  The row tiles
     // move down through the first one's registers.
 #pragma unroll 1
     for (int t = 0; t < RT; ++t) {
+        if (fetch && t % 2 == 0) {
+#pragma unroll 1
+            for (int u = 0; u < 2 * PIECES; ++u) {      // (rows past the last: zeros)
+                const int r = (wr * RT + t) * MI + u * RPP + lane / LPR;
+                const uint32_t off = r < rows_valid && j < p.n ? (uint32_t)((r * ld_other + j - col0) * 2) : OOB;
+                lds_dma<16>(o_rsrc, fetched + u * 1024, off);
+            }
+        }
 #pragma unroll
         for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -369,6 +390,10 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
                     turn[r * CP + (g * CT + c) * MI + lane % MI] = acc[g][0][c][e];
                 }
         asm volatile("" ::: "memory");
+        if (fetch && t % 2 == 0) {
+            __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8) | (0 << 14));     // vmcnt(0)
+            asm volatile("" ::: "memory");
+        }
 #pragma unroll 1
         for (int r = lane / LPR; r < MI; r += RPP) {
             const int64_t i = row0 + (wr * RT + t) * MI + r;
@@ -377,7 +402,8 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
             if (i < p.m && j < p.n) {
                 if (p.splits > 1) store_row<8, true>(p.part + ((int64_t)split * p.m + i) * p.n + j, 8, x);
                 else if (p.epi.f32) half_store8<float>(p.epi, i, j, x);
-                else half_store8<T>(p.epi, i, j, x);
+                else half_store8<T>(p.epi, i, j, x, fetch ? reinterpret_cast<const T *>(
+                         fetched + (t % 2 * PIECES + r / RPP) * 1024 + lane * 16) : nullptr);
             }
         }
         asm volatile("" ::: "memory");
