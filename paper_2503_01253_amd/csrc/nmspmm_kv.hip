@@ -466,9 +466,16 @@ AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_
     int64_t span = std::min(max_length, table_positions(c));
     if (window > 0) span = std::min(span, window);
     const int64_t base = c->sequences * c->heads * a.gtiles;
-    // eight workgroups a CU (two or three run at once), each of 256 positions at least
+    // eight workgroups a CU (two or three run at once), each of 256 positions at
+    // least; and of 1024 at most, for batches whose lengths differ, which only
+    // the device knows (192 sequences of 0 to 5000 positions, 64 heads on 8: 273
+    // us, with chunks of 2500 404; 64 of 8192 each: 420 and 407), up to 64
+    // workgroups a CU (which bounds the workspace)
     int64_t splits = 1;
-    if (split && base > 0) splits = std::max<int64_t>(1, std::min<int64_t>((JN_SPLITS + base - 1) / base, span / 256));
+    if (split && base > 0) {
+        splits = std::max<int64_t>(1, std::min<int64_t>((JN_SPLITS + base - 1) / base, span / 256));
+        splits = std::max(splits, std::min<int64_t>({JN_SPLITS, (span + 1023) / 1024, 16384 / base}));
+    }
     a.chunk = (int)std::min<int64_t>(INT31 - 127, std::max<int64_t>(128, ((span + splits - 1) / splits + 127) / 128 * 128));
     a.splits = (int)std::max<int64_t>(1, (span + a.chunk - 1) / a.chunk);
     a.groups = base * a.splits;
