@@ -70,6 +70,7 @@ struct AttendArgs {
     int32_t heads, group, gtiles, dim, splits, chunk;
     float scale2;               // scale * log2(e): exponentials are powers of 2
     nmspmm_dtype_t io;
+    bool q_vec;                 // the queries' rows start on 16 bytes
 };
 
 // One workgroup's work: a tile of query heads of one cache head of one

@@ -663,6 +663,7 @@ extern "C" nmspmm_status_t nmspmm_kv_attend(const nmspmm_kv_cache_t *cache, cons
     p.chunk = a.chunk;
     p.scale2 = scale * 1.44269504089f;
     p.io = dtype;
+    p.q_vec = rows_aligned(q, q_stride, 2, cache->dim, es);
     const int cs = dtype_bytes(cache->dtype);
     const bool vec = rows_aligned(cache->k_pages, cache->k_stride, 3, cache->dim, cs) &&
                      rows_aligned(cache->v_pages, cache->v_stride, 3, cache->dim, cs);

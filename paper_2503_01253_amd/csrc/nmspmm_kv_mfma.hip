@@ -102,6 +102,13 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 && QP == 1 ? 3 : DK <= 4 ? 2 : 1) vo
             const bool there = col < t.heads_in_tile && d < p.dim;
             const int64_t at = t.seq * p.qs[0] + (t.first_head + col) * p.qs[1] + d;
             if constexpr (QP == 1) {
+                if (p.q_vec) {      // eight at once
+                    if (j == 0) {
+                        q[0][c] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                        if (there) q[0][c] = *reinterpret_cast<const s16x8 *>(static_cast<const short *>(p.q) + at);
+                    }
+                    continue;
+                }
                 q[0][c][j] = there ? static_cast<const short *>(p.q)[at] : (short)0;
             } else {
                 const float x = !there ? 0.f : p.io == NMSPMM_F32 ? static_cast<const float *>(p.q)[at]
