@@ -173,7 +173,8 @@ NMSPMM_API int64_t nmspmm_kv_attend_workspace_bytes(const nmspmm_kv_cache_t *cac
  *            denominator (to join results over parts of a context), or NULL
  * A position whose page lies outside the cache is left out.  Positions outside
  * the range are not read into any sum: what their slots hold (NaN, say) does
- * not matter.  Scores, softmax and sums are fp32; out is rounded once.  The
+ * not matter.  An infinity inside it makes the sums it enters infinite or NaN.
+ * Scores, softmax and sums are fp32; out is rounded once.  The
  * order of summation is fixed by shapes, lengths and workspace.  No sequences
  * or no query heads: NMSPMM_OK without a launch.  Errors:
  * NMSPMM_ERR_INVALID_ARG (negative size, bad type, q_heads no multiple of

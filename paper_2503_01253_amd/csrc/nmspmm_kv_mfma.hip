@@ -158,6 +158,9 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 && QP == 1 ? 3 : DK <= 4 ? 2 : 1) vo
         }
     };
 
+    // fp16's smallest step is 2^-24, which weights of at most 1 come near in a long
+    // sequence: they are held times 2^14 there, sums and values alike
+    constexpr float LIFT = __is_same(T, f16_t) ? 0x1p14f : 1.f, LOWER = 1.f / LIFT;
     f32x4 o[DK * 2];
 #pragma unroll
     for (int b = 0; b < DK * 2; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -205,7 +208,7 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 && QP == 1 ? 3 : DK <= 4 ? 2 : 1) vo
         s16x8 w[PP];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float e = __builtin_amdgcn_exp2f(x[j] - ref);
+            const float e = __builtin_amdgcn_exp2f(x[j] - ref) * LIFT;
             l += e;
             short part[PP];
             split_parts<T, PP>(e, part);
@@ -235,12 +238,12 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 && QP == 1 ? 3 : DK <= 4 ? 2 : 1) vo
     }
 
     // ---- the four waves joined ----
-    l = across_groups(l, [](float a, float b) { return a + b; });
+    l = across_groups(l, [](float a, float b) { return a + b; }) * LOWER;
     __syncthreads();
     float *acc = reinterpret_cast<float *>(lds);
 #pragma unroll
     for (int b = 0; b < DK * 2; ++b)
-        *reinterpret_cast<f32x4 *>(acc + (wave * GT + col) * AP + b * 16 + grp * 4) = o[b];
+        *reinterpret_cast<f32x4 *>(acc + (wave * GT + col) * AP + b * 16 + grp * 4) = o[b] * LOWER;
     if (grp == 0) s_ml[wave][col] = make_float2(m, l);
     __syncthreads();
     for (int i = threadIdx.x; i < t.heads_in_tile * p.dim; i += AM_NT) {

@@ -365,3 +365,27 @@ def test_streams_graphs_and_determinism(dtype, cache):
         assert torch.equal(out, first)
         tol = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -14      # one split or several: the order of the sums
         assert torch.all((bare_out.float() - first.float()).abs() <= tol * (first.float().abs() + 0.1))
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("f16", "f16"), ("f32", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("first", [0, 1, 199])
+def test_many_weights_below_half_a_step(first, dtype, cache):
+    """One position 17.5 above the others, whose values are zero: the others'
+    weights, e^-17.5 each, lie below half of fp16's smallest step, and they make
+    the whole result.  It is at most 2^-15 of itself off (each weight two parts
+    of 16 bits) before its rounding."""
+    say(f"[kv] small weights {first} {dtype} {cache}")
+    dim, length, page = 64, 200, 8
+    k = torch.zeros(25, page, 1, dim)
+    v = torch.full((25, page, 1, dim), 1000.0)
+    k[first // page, first % page, 0, 0] = 17.5
+    v[first // page, first % page] = 0.0
+    handle = nm.nmspmm_kv_cache(k.to(DTYPES[cache]).cuda(), v.to(DTYPES[cache]).cuda(),
+                                torch.arange(25, dtype=torch.int32, device="cuda").view(1, 25))
+    q = torch.zeros(1, 3, dim)
+    q[..., 0] = 1.0
+    out = torch.empty(1, 3, dim, dtype=DTYPES[dtype], device="cuda")
+    nm.nmspmm_kv_attend(handle, q.to(DTYPES[dtype]).cuda(), torch.tensor([length]).int().cuda(), out, scale=1.0)
+    small = (length - 1) * np.exp(-17.5)
+    want = 1000.0 * small / (1.0 + small)
+    assert np.all(np.abs(f64(out) - want) <= (2.0 ** -15 + ROUND[dtype]) * want)
