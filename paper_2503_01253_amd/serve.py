@@ -95,15 +95,15 @@ def _shape(name, t, shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
-def _workspace(t, device):
+def _workspace(t, device, name="workspace"):
     """Address and size of a workspace tensor, or nothing."""
     if t is None:
         return None, 0
     import torch
     if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous():
-        raise TypeError("workspace must be a contiguous CUDA tensor of torch.uint8")
+        raise TypeError(f"{name} must be a contiguous CUDA tensor of torch.uint8")
     if t.device != device:
-        raise ValueError(f"workspace is on {t.device}, {device} expected")
+        raise ValueError(f"{name} is on {t.device}, {device} expected")
     return t.data_ptr(), t.numel()
 
 
@@ -112,8 +112,14 @@ class HalfWeight:
 
     def __init__(self, packed, dtype, k, n, N, M, V):
         _library()
-        if dtype not in _dtypes:
+        if _dtypes.get(dtype) not in (NMSPMM_BF16, NMSPMM_F16):
             raise TypeError(f"dtype must be torch.bfloat16 or torch.float16, not {dtype}")
+        size, held = nmspmm_half_bytes(k, n, N, M, V), _workspace(packed, getattr(packed, "device", None), "packed")[1]
+        if size < 0:
+            raise binding.NmSpmmError("HalfWeight", binding.NMSPMM_ERR_INVALID_ARG,
+                                      f"invalid shape k={k} n={n} N={N} M={M} V={V}")
+        if held < size:
+            raise ValueError(f"packed has {held} bytes, {size} needed")
         self.packed, self.dtype, self.device, self.at = packed, dtype, packed.device, packed.get_device()
         self.k, self.n, self.N, self.M, self.V = k, n, N, M, V
         self._c = _Weight(packed.data_ptr(), _dtypes[dtype], N, M, V, k, n)
@@ -151,7 +157,7 @@ def nmspmm_half_pack(Bc, idx, n: int, k: int, N: int, M: int, V: int, dtype=None
         packed = torch.empty(size, dtype=torch.uint8, device=Bc.device)
         if stream is not None:
             packed.record_stream(stream)
-    elif _workspace(packed, Bc.device)[1] < size:
+    elif _workspace(packed, Bc.device, "packed")[1] < size:
         raise ValueError(f"packed has {packed.numel()} bytes, {size} needed")
     weight = HalfWeight(packed, dtype, k, n, N, M, V)
     st = _call(torch, at, L.nmspmm_half_pack, Bc.data_ptr(), _dtypes[Bc.dtype], idx.data_ptr(), weight._ref,

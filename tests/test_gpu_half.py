@@ -291,3 +291,19 @@ def test_streams_graphs_and_determinism(m):
         nm.nmspmm_half_run(A, weight, C, residual=residual)
         torch.cuda.synchronize()
         assert torch.equal(C, first)
+
+
+def test_handle_refuses_what_is_no_packed_weight():
+    size = nm.nmspmm_half_bytes(256, 64, 8, 32, 32)
+    packed = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    assert nm.HalfWeight(packed, torch.bfloat16, 256, 64, 8, 32, 32).k == 256
+    with pytest.raises(ValueError):
+        nm.HalfWeight(packed[:-1], torch.bfloat16, 256, 64, 8, 32, 32)
+    with pytest.raises(TypeError):
+        nm.HalfWeight(packed, torch.float32, 256, 64, 8, 32, 32)
+    with pytest.raises(TypeError):
+        nm.HalfWeight(packed.float(), torch.bfloat16, 256, 64, 8, 32, 32)
+    with pytest.raises(TypeError):
+        nm.HalfWeight(packed.cpu(), torch.bfloat16, 256, 64, 8, 32, 32)
+    with pytest.raises(nm.NmSpmmError):
+        nm.HalfWeight(packed, torch.bfloat16, 250, 64, 8, 32, 32)
