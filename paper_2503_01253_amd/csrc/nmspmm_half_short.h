@@ -69,6 +69,7 @@ __global__ __launch_bounds__(HS_NT, SLOT == HS_SLOT ? 4 : 2) void nm_half_short_
 
     // ---- A: a few waves a row, or a few rows a wave ----
     const int row_bytes = p.chunk_units * p.KR * 2, pitch = half_short_pitch(p.chunk_units, p.KR);
+    // (k is a multiple of 8 here, of whole units, so no row ends inside a word)
     const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(p.A, (uint32_t)(((p.m - 1) * p.lda + p.k) * 2));
     const int share = p.m == 1 ? 3 : p.m == 2 ? 2 : p.m <= 4 ? 1 : 0;      // log2 of the waves of a row
     auto load_a = [&](int chunk, int slot) {

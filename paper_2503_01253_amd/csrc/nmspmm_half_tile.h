@@ -143,9 +143,12 @@ __global__ __launch_bounds__(C::NT, C::WPS) void nm_half_tile_kernel(HalfTileArg
     const int kstage = p.P * p.KR, slot_bytes = p.P * (p.KR + 1) * PITCH;
     const int rows_valid = (int)min64(BM, p.m - row0);
     // (rows past the last and columns past k read zeros or a neighbour's
-    // values: the former's outputs are not stored, no offset leads to the latter)
+    // values: the former's outputs are not stored, no offset leads to the latter.
+    // Wide loads are checked by whole words of 4 bytes: an odd k's last value
+    // needs the word it lies in, which starts inside A)
+    const uint32_t a_bytes = (uint32_t)(((rows_valid - 1) * p.lda + p.k) * 2);
     const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(static_cast<const T *>(p.A) + row0 * p.lda,
-                                                    (uint32_t)(((rows_valid - 1) * p.lda + p.k) * 2));
+                                                    VEC ? (a_bytes + 3) & ~3u : a_bytes);
     u32x4 ra[AD][NB][4];
     uint32_t a_off[NB], a_dst[NB];
     // block b of this thread: rows 4*rb.., columns 8*kc.. of the stage.  A wave

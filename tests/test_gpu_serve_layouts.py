@@ -98,3 +98,26 @@ def test_queries_at_any_place(dim, dtype, cache):
     nm.nmspmm_kv_attend(handle, turned, lengths, turned_out)
     torch.cuda.synchronize()
     assert torch.equal(odd_out, out) and torch.equal(turned_out, out)
+
+
+@pytest.mark.parametrize("shape", [
+    # m, k, n, N, M, V: k of no whole pieces of eight
+    (1, 243, 64, 4, 9, 32), (1, 27, 32, 4, 9, 32), (33, 243, 64, 4, 9, 32), (130, 45, 96, 3, 5, 32),
+    (3, 770, 96, 1, 77, 32), (1, 12, 32, 2, 4, 32), (16, 52, 64, 2, 4, 32), (40, 84, 48, 2, 4, 16),
+    (1, 90, 48, 8, 10, 16), (2, 88, 32, 8, 8, 32), (1, 5, 16, 5, 5, 16), (70, 35, 32, 7, 7, 32), (1, 1, 32, 1, 1, 32),
+    (9, 4, 32, 4, 4, 32), (17, 66, 32, 8, 22, 32)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_last_columns_of_a_beside_nothing(shape, dtype):
+    """A's rows start on 16 bytes and end inside a piece of eight: the last
+    columns count, and NaN between them and the next row does not."""
+    say(f"[layout] ends {shape} {dtype}")
+    m, k, n, N, M, V = shape
+    A, weight, want = product(*shape, dtype=dtype)
+    for stride in (k, (k + 7) // 8 * 8, (k + 7) // 8 * 8 + 8):
+        flat = torch.full(((m - 1) * stride + k + 64,), float("nan"), dtype=dtype, device="cuda")
+        rows = torch.as_strided(flat, (m, k), (stride, 1))
+        rows.copy_(A)
+        C = torch.full_like(want, float("nan"))
+        nm.nmspmm_half_run(rows, weight, C)
+        torch.cuda.synchronize()
+        assert torch.equal(C, want)
