@@ -497,6 +497,7 @@ bool attend_takes_mfma(const nmspmm_kv_cache_t *c, nmspmm_dtype_t dtype)
         const int64_t limit = (int64_t)1 << 34;     // elements: 2^32 - 1 pieces hold every row's start
         if (stride[0] < 0 || stride[1] < 0 || stride[0] > limit || stride[1] > limit) return false;
         if (stride[0] && c->pages > limit / stride[0]) return false;
+        if (stride[1] && c->page_size > limit / stride[1]) return false;
         if (c->pages * stride[0] + c->page_size * stride[1] > limit) return false;
     }
     return rows_aligned(c->k_pages, c->k_stride, 3, c->dim, 2) && rows_aligned(c->v_pages, c->v_stride, 3, c->dim, 2);
