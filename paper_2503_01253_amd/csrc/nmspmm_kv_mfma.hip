@@ -7,17 +7,24 @@
 //   S^T = K Q^T   v_mfma_f32_16x16x32: A operand 16 tokens, read from memory
 //                 as its lanes hold them (16 bytes of a token's row a lane),
 //                 B operand the queries, kept in registers;
+//                 Queries that are not bf16 over a bf16 cache: three bf16 parts
+//                 of every query value, which hold all 24 bits (a batch of
+//                 42 x 676 positions, 7 heads of 256, 87 us on the vector ALU);
 //   P^T           running maximum of each head (a lane's column), weights in
-//                 fp32, each as two 16-bit parts (2^-17 of itself together;
-//                 one part alone would double the error of a 16-bit output);
-//                 queries that are not bf16 over a bf16 cache: three bf16 parts
-//                 of every query value and of every weight, which hold all 24
-//                 bits (a batch of 42 x 676 positions, 7 heads of 256, 87 us on
-//                 the vector ALU);
+//                 fp32;
 //   O^T += V^T P^T  the weights lie in the lanes just as the B operand wants
 //                 them (k index 8g+j stands for token 4g+j, or 16+4g+j-4 from
 //                 j = 4 on); V goes through LDS, a wave's own piece, whose
 //                 transposed reads give V^T.
+// A weight enters in 16-bit parts that keep fp32's precision.  bf16: three, all
+// 24 bits (two left up to 2^-17 out, which turned single bf16 results; three
+// are no slower).  fp16, whose smallest step a long sequence's weights come near:
+// two of the weight times 2^14, which leave at most 2^-22 out from 2^-17 of the
+// maximum on; where a tile has smaller weights, two more of what is left, times
+// 2^24, so that what is lost lies under the rounding of any fp16 result.  (64
+// sequences of 4096, 8 heads of 128, fp16: 212 us, 214 where most tiles have
+// small weights; with V converted and the weights as they are on
+// v_mfma_f32_16x16x4_f32 219, 32 ragged sequences of 4 heads of 256 82, 88 and 99.)
 // The next tokens' K is on its way while the weights form, the next V while
 // it is multiplied.  The waves are joined in LDS.  Bound by HBM: 128 x 8192
 // positions, 32 heads on 8 of 128, 771 us (5.6 TB/s), one sequence of 131071
@@ -48,9 +55,10 @@ __device__ __forceinline__ f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c)
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// x as PARTS 16-bit values, each the nearest to what those before it leave.
+// x as PARTS 16-bit values, each the nearest to what those before it leave;
+// returns what they all leave.
 template <class T, int PARTS>
-__device__ __forceinline__ void split_parts(float x, short (&part)[PARTS])
+__device__ __forceinline__ float split_parts(float x, short *part)
 {
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) {
@@ -58,6 +66,7 @@ __device__ __forceinline__ void split_parts(float x, short (&part)[PARTS])
         part[i] = __builtin_bit_cast(short, h);
         x -= to_f32(h);
     }
+    return x;
 }
 
 // The values of the lanes 16 and 32 away: after the swap one result holds the
@@ -73,11 +82,20 @@ __device__ __forceinline__ float across_groups(float x, F f)
     return f(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
 }
 
+// Workgroups of a CU: as many as its registers hold (with three, the fp16 kernel
+// for 128 dimensions kept registers in memory: 64 x 4096 positions 374 us, with
+// two 212).
+constexpr int attend_groups(bool f16, int DK, int QP) { return DK > 4 ? 1 : QP > 1 || (DK > 2 && f16) ? 2 : 3; }
+
 // DK: pieces of 32 dimensions.  QP: parts of a query value.
 template <class T, int DK, int QP>
-__global__ __launch_bounds__(AM_NT, DK <= 4 && QP == 1 ? 3 : DK <= 4 ? 2 : 1) void nm_attend_mfma_kernel(AttendArgs p)
+__global__ __launch_bounds__(AM_NT, attend_groups(__is_same(T, f16_t), DK, QP)) void nm_attend_mfma_kernel(AttendArgs p)
 {
-    constexpr int PP = QP == 1 ? 2 : 3;     // parts of a weight
+    constexpr bool F16 = __is_same(T, f16_t);
+    constexpr int PP = F16 ? 2 : 3;     // parts of a weight
+    // what an fp16 weight's parts are multiplied by, what the two parts of their
+    // rest are beside that, and the weight from which on no rest is needed
+    constexpr float LIFT = F16 ? 0x1p14f : 1.f, REST = 0x1p24f, WHOLE = 0x1p-17f;
     constexpr int GT = 16, CPR = DK * 4, VL = CPR / 2, VPITCH = DK * 64 + 32, AP = DK * 32 + 4;
     static_assert(AM_NW * GT * AP * 4 <= AM_NW * AM_TOKENS * VPITCH, "the joining of the waves");
     __shared__ __align__(16) unsigned char lds[AM_NW * AM_TOKENS * VPITCH];
@@ -158,9 +176,6 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 && QP == 1 ? 3 : DK <= 4 ? 2 : 1) vo
         }
     };
 
-    // fp16's smallest step is 2^-24, which weights of at most 1 come near in a long
-    // sequence: they are held times 2^14 there, sums and values alike
-    constexpr float LIFT = __is_same(T, f16_t) ? 0x1p14f : 1.f, LOWER = 1.f / LIFT;
     f32x4 o[DK * 2];
 #pragma unroll
     for (int b = 0; b < DK * 2; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -168,6 +183,15 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 && QP == 1 ? 3 : DK <= 4 ? 2 : 1) vo
     unsigned char *vs = lds + wave * (AM_TOKENS * VPITCH);
     const uint32_t vt = (uint32_t)(uintptr_t)(lds_u8 *)(lds_void *)vs +
                         (uint32_t)((grp * 4 + ((lane >> 2) & 3)) * VPITCH + (lane & 3) * 8);
+
+    // dimensions 16 b and on of the tile's V^T, as the A operand's lanes hold them
+    auto values = [&](int b) {
+        s16x4 v[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+            v[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(lds_u8 *)(uintptr_t)(vt + b * 32 + y * 16 * VPITCH));
+        return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
 
     int base = t.begin + wave * AM_TOKENS;
     Rows cur = look_up(base), next = look_up(base + AM_NW * AM_TOKENS);
@@ -206,12 +230,15 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 && QP == 1 ? 3 : DK <= 4 ? 2 : 1) vo
             m = top;
         }
         s16x8 w[PP];
+        float left[8];
+        bool small = false;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float e = __builtin_amdgcn_exp2f(x[j] - ref) * LIFT;
             l += e;
+            small |= e > 0.f && e < WHOLE * LIFT;
             short part[PP];
-            split_parts<T, PP>(e, part);
+            left[j] = split_parts<T, PP>(e, part);
 #pragma unroll
             for (int i = 0; i < PP; ++i) w[i][j] = part[i];
         }
@@ -227,23 +254,35 @@ __global__ __launch_bounds__(AM_NT, DK <= 4 && QP == 1 ? 3 : DK <= 4 ? 2 : 1) vo
         next = look_up(base + 2 * AM_NW * AM_TOKENS);
 #pragma unroll
         for (int b = 0; b < DK * 2; ++b) {
-            s16x4 v[2];
-#pragma unroll
-            for (int y = 0; y < 2; ++y)
-                v[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(lds_u8 *)(uintptr_t)(vt + b * 32 + y * 16 * VPITCH));
-            const s16x8 a = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+            const s16x8 a = values(b);
 #pragma unroll
             for (int i = PP - 1; i >= 0; --i) o[b] = mfma16<T>(a, w[i], o[b]);
+        }
+        if (F16 && __any(small)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                short part[2];
+                split_parts<T, 2>(left[j] * REST, part);
+                w[0][j] = part[0];
+                w[1][j] = part[1];
+            }
+#pragma unroll
+            for (int b = 0; b < DK * 2; ++b) {
+                const s16x8 a = values(b);
+                const f32x4 rest = mfma16<T>(a, w[0], mfma16<T>(a, w[1], f32x4{0.f, 0.f, 0.f, 0.f}));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[b][i] = fmaf(rest[i], 1.f / REST, o[b][i]);
+            }
         }
     }
 
     // ---- the four waves joined ----
-    l = across_groups(l, [](float a, float b) { return a + b; }) * LOWER;
+    l = across_groups(l, [](float a, float b) { return a + b; }) / LIFT;
     __syncthreads();
     float *acc = reinterpret_cast<float *>(lds);
 #pragma unroll
     for (int b = 0; b < DK * 2; ++b)
-        *reinterpret_cast<f32x4 *>(acc + (wave * GT + col) * AP + b * 16 + grp * 4) = o[b] * LOWER;
+        *reinterpret_cast<f32x4 *>(acc + (wave * GT + col) * AP + b * 16 + grp * 4) = o[b] / LIFT;
     if (grp == 0) s_ml[wave][col] = make_float2(m, l);
     __syncthreads();
     for (int i = threadIdx.x; i < t.heads_in_tile * p.dim; i += AM_NT) {
