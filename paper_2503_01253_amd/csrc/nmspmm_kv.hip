@@ -14,6 +14,7 @@ bool aligned_to(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t
 
 constexpr int64_t INT31 = 0x7fffffff;
 constexpr int KV_MAX_DIM = 512;
+constexpr int64_t KV_MAX_LENGTH = INT31 - 4096;     // the kernels step a few hundred positions past the last
 
 nmspmm_status_t check_cache(const nmspmm_kv_cache_t *c)
 {
@@ -463,7 +464,7 @@ AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_
     const int64_t group = q_heads / c->heads;
     a.GT = mfma ? ATTEND_MFMA_HEADS : group >= 5 ? 8 : group >= 3 ? 4 : (int)group;
     a.gtiles = (int)((group + a.GT - 1) / a.GT);
-    int64_t span = std::min(max_length, table_positions(c));
+    int64_t span = std::min({max_length, table_positions(c), KV_MAX_LENGTH});
     if (window > 0) span = std::min(span, window);
     const int64_t base = c->sequences * c->heads * a.gtiles;
     // eight workgroups a CU (two or three run at once), each of 256 positions at
@@ -476,8 +477,8 @@ AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_
         splits = std::max<int64_t>(1, std::min<int64_t>((JN_SPLITS + base - 1) / base, span / 256));
         splits = std::max(splits, std::min<int64_t>({JN_SPLITS, (span + 1023) / 1024, 16384 / base}));
     }
-    a.chunk = (int)std::min<int64_t>(INT31 - 127, std::max<int64_t>(128, ((span + splits - 1) / splits + 127) / 128 * 128));
-    a.splits = (int)std::max<int64_t>(1, (span + a.chunk - 1) / a.chunk);
+    a.chunk = (int)std::max<int64_t>(128, ((span + splits - 1) / splits + 127) / 128 * 128);
+    a.splits = (int)std::max<int64_t>(1, (span + a.chunk - 1) / a.chunk);     // 1 where splits is
     a.groups = base * a.splits;
     a.rows = c->sequences * q_heads;
     if (a.splits > 1) {
@@ -653,8 +654,7 @@ extern "C" nmspmm_status_t nmspmm_kv_attend(const nmspmm_kv_cache_t *cache, cons
         p.qs[i] = q_stride[i];
         p.os[i] = out_stride[i];
     }
-    // (the kernels step a few hundred positions past the last)
-    p.cap = (int)std::min({max_length, table_positions(cache), INT31 - 4096});
+    p.cap = (int)std::min({max_length, table_positions(cache), KV_MAX_LENGTH});
     p.window = (int)std::min(window, INT31);
     p.heads = cache->heads;
     p.group = (int)(q_heads / cache->heads);

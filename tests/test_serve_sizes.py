@@ -1,0 +1,26 @@
+"""CPU tests of the sizes that the decoding-step operators plan with, at the
+ends of what their ABI takes: no kernel is launched."""
+import ctypes
+
+import pytest
+
+import paper_2503_01253_amd as nm
+from paper_2503_01253_amd import serve
+
+PTR = 1 << 20      # an address that is never used
+
+
+@pytest.mark.parametrize("window", [0, 2 ** 31 - 1, 2 ** 40])
+@pytest.mark.parametrize("table_pages,page_size", [
+    (32767, 65536), (1, 2 ** 31 - 128), (1, 2 ** 31 - 127), (1, 2 ** 31 - 1), (32768, 65536), (2 ** 31 - 1, 1),
+    (2 ** 31 - 1, 2 ** 31 - 1), (1, 2 ** 31 - 4097), (1, 2 ** 31 - 4096)])
+def test_attend_that_does_not_split_needs_no_workspace(table_pages, page_size, window):
+    """Enough sequences to fill the GPU without splitting any: no workspace,
+    however many positions the table names (a second split without one would
+    be written nowhere)."""
+    strides = (ctypes.c_int64 * 3)(0, 0, 64)
+    cache = ctypes.pointer(serve._Cache(PTR, PTR, strides, strides, 1, PTR, table_pages, 20000, table_pages, page_size,
+                                        1, 64, nm.NMSPMM_BF16))
+    size = serve._library().nmspmm_kv_attend_workspace_bytes
+    for max_length in (table_pages * page_size, 2 ** 31 - 129, 2 ** 31 - 1, 2 ** 40, 2 ** 62):
+        assert size(cache, 1, max_length, window) == 0, max_length
