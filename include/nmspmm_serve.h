@@ -69,7 +69,8 @@ typedef enum {
 } nmspmm_half_act_t;
 
 /* Bytes of workspace with which nmspmm_half_run splits k for a product of m
- * rows: 0 where it does not, -1 for a bad shape.  Host only. */
+ * rows, wherever A's rows start (rows on 16 bytes may need fewer): 0 where it
+ * does not, -1 for a bad shape.  Host only. */
 NMSPMM_API int64_t nmspmm_half_workspace_bytes(int64_t m, const nmspmm_half_weight_t *weight);
 
 /* The sparse product of nmspmm.h (Eq. 1) with 16-bit operands:
@@ -98,8 +99,8 @@ NMSPMM_API nmspmm_status_t nmspmm_half_run(const void *A, int64_t lda, const nms
                                 int64_t ld_residual, void *workspace, size_t workspace_bytes,
                                 hipStream_t stream);
 
-/* Name of the kernel that nmspmm_half_run launches for m rows, with a
- * workspace or without ("none": no launch, "invalid": bad shape), for reports.
+/* Name of the kernel that nmspmm_half_run launches for m rows that start on 16
+ * bytes (others may take another), with a workspace or without ("none": no launch, "invalid": bad shape), for reports.
  * Valid until the thread's next call. */
 NMSPMM_API const char *nmspmm_half_kernel_name(int64_t m, const nmspmm_half_weight_t *weight, int with_workspace);
 

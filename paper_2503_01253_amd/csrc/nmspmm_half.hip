@@ -509,7 +509,8 @@ extern "C" int64_t nmspmm_half_workspace_bytes(int64_t m, const nmspmm_half_weig
     if (check_weight(weight, m) != NMSPMM_OK) return -1;
     if (m == 0 || weight->n == 0) return 0;
     const HalfLayout l = half_layout(weight->k, weight->n, weight->N, weight->M, weight->V);
-    return half_plan(m, l, *weight, true, true).ws_bytes;
+    // of whichever plan A's place will choose
+    return std::max(half_plan(m, l, *weight, true, true).ws_bytes, half_plan(m, l, *weight, false, true).ws_bytes);
 }
 
 extern "C" const char *nmspmm_half_kernel_name(int64_t m, const nmspmm_half_weight_t *weight, int with_workspace)

@@ -24,3 +24,15 @@ def test_attend_that_does_not_split_needs_no_workspace(table_pages, page_size, w
     size = serve._library().nmspmm_kv_attend_workspace_bytes
     for max_length in (table_pages * page_size, 2 ** 31 - 129, 2 ** 31 - 1, 2 ** 40, 2 ** 62):
         assert size(cache, 1, max_length, window) == 0, max_length
+
+
+@pytest.mark.parametrize("m,k,n,N,M,V", [(1, 8192, 256, 4, 32, 64), (8, 4096, 4096, 8, 32, 32), (16, 8192, 512, 16, 32, 32),
+                                         (3, 4096, 64, 8, 32, 16)])
+def test_half_workspace_counts_rows_of_a_off_16_bytes(m, k, n, N, M, V):
+    """Rows on 16 bytes take the kernel of few rows, which needs no workspace;
+    others cut k into slices, and one size has to hold for both."""
+    weight = ctypes.pointer(serve._Weight(PTR, nm.NMSPMM_BF16, N, M, V, k, n))
+    L = serve._library()
+    assert L.nmspmm_half_kernel_name(m, weight, 1).startswith(b"nm_half_short_kernel")
+    size = L.nmspmm_half_workspace_bytes(m, weight)
+    assert size >= 2 * m * n * 4 and size % (m * n * 4) == 0
