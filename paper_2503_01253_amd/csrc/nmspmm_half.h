@@ -27,7 +27,8 @@ struct HalfEpilogue {
 __device__ __forceinline__ float half_act(float y, int act)
 {
     if (act == NMSPMM_HALF_ACT_RELU) return y < 0.f ? 0.f : y;      // NaN stays NaN
-    if (act == NMSPMM_HALF_ACT_GELU) return 0.5f * y * (1.f + erff(y * 0.70710678118f));
+    // erfc, not 1 + erf, of which nothing is left below y = -5.5
+    if (act == NMSPMM_HALF_ACT_GELU) return 0.5f * y * erfcf(y * -0.70710678118f);
     if (act == NMSPMM_HALF_ACT_SILU) return y / (1.f + __expf(-y));
     return y;
 }
