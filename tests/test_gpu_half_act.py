@@ -76,3 +76,16 @@ def test_gelu_times_a_large_factor(out):
     tol = np.abs(want) * (ROUND[out] + 2.0 ** -16) + (2.0 ** -25 if out == "f16" else 0)
     err = np.abs(results(y, "gelu", 40, True, out, 32768.0) - want)
     assert np.all(err <= tol), f"worst {np.max(err / tol)} of the tolerance"
+
+
+@pytest.mark.parametrize("vector", [False, True])
+@pytest.mark.parametrize("m", [1, 40, 300])
+def test_silu(m, vector):
+    print(f"[half act] silu {m} {vector}", file=sys.stderr, flush=True)
+    for lo, hi in ((-86, -30), (-30, -3), (-3, 3), (3, 100)):
+        y = values(lo, hi)
+        y64 = y.astype(np.float64)
+        want = y64 * np.where(y64 < 0, np.exp(y64), 1) / (1 + np.exp(-np.abs(y64)))
+        tol = np.abs(want) * 8 * 2.0 ** -24 + 2.0 ** -126
+        err = np.abs(results(y, "silu", m, vector) - want)
+        assert np.all(err <= tol), f"{lo} to {hi}: worst {np.max(err / tol)} of the tolerance at {y[np.argmax(err / tol)]}"
