@@ -42,7 +42,8 @@ __device__ __forceinline__ float half_act(float y, int act)
     // erfc, not 1 + erf, of which nothing is left below y = -5.5
     if (act == NMSPMM_HALF_ACT_GELU) return 0.5f * y * erfcf(y * -0.70710678118f);
     if (act == NMSPMM_HALF_ACT_SILU) {
-        const float t = half_exp(-fabsf(y)), d = 1.f + t;       // of -|y|: no overflow
+        // of -|y|: no overflow; below -104 it is 0 (and an infinity's is not NaN)
+        const float t = half_exp(fmaxf(-fabsf(y), -104.f)), d = 1.f + t;
         const float r = __builtin_amdgcn_rcpf(d);               // and a step of Newton's: d is 1 to 2
         return y * ((y < 0.f ? t : 1.f) * fmaf(r, fmaf(-d, r, 1.f), r));
     }

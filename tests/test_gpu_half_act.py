@@ -89,3 +89,15 @@ def test_silu(m, vector):
         tol = np.abs(want) * 8 * 2.0 ** -24 + 2.0 ** -126
         err = np.abs(results(y, "silu", m, vector) - want)
         assert np.all(err <= tol), f"{lo} to {hi}: worst {np.max(err / tol)} of the tolerance at {y[np.argmax(err / tol)]}"
+
+
+@pytest.mark.parametrize("vector", [False, True])
+@pytest.mark.parametrize("m", [1, 40])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+def test_infinities_and_nan(act, m, vector):
+    """Plus infinity stays, NaN stays, and what is finite beside them does."""
+    y = np.ones(64, np.float32)
+    y[3], y[10], y[20], y[21] = np.inf, np.nan, 3e38, -3e38
+    got = results(y, act, m, vector)
+    assert got[3] == np.inf and np.isnan(got[10]) and np.isfinite(np.delete(got, [3, 10])).all()
+    assert got[20] == np.float64(y[20]) and got[21] == (np.float64(y[21]) if act == "none" else 0)
