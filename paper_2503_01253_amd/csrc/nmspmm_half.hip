@@ -286,8 +286,8 @@ struct HalfPlan {
 // barrier, the latencies of its loads and reads), and where the CU is full
 // what it loads from L2 (134 bytes a ns), writes into LDS (100, 32-row tiles
 // half that) and multiplies (6.45 GFLOP/s a CU) take their time one after
-// another.  (Fitted on MI355X: 4096^3 at 16:32 and V = 64 128 x 256 tiles 89 us
-// measured, 96 estimated; 128 x 128 118 and 131; 37 x 4096 x 11008 at 8:32 64 x 64 tiles 15.6 and
+// another.  (Fitted on MI355X: 4096^3 at 16:32 and V = 64 128 x 256 tiles, CT = 1,
+// 94 us measured, 96 estimated; 128 x 128 114 and 131; 37 x 4096 x 11008 at 8:32 64 x 64 tiles 15.6 and
 // 15.8, 64 x 128 17.3 and 16.4; 128 x 4096 x 4096 at 16:32 32 x 64 13.0 and
 // 11.7, 64 x 64 17.6 and 16.4.)
 double half_cost(const HalfTileInfo &t, const HalfLayout &l, int P, int QS, int64_t workgroups, int stages)
@@ -526,8 +526,8 @@ extern "C" const char *nmspmm_half_kernel_name(int64_t m, const nmspmm_half_weig
         return buf;
     }
     const HalfTileInfo &t = half_tiles[c.tile];
-    std::snprintf(buf, sizeof buf, "nm_half_tile_kernel<%dx%d,mi%d,wk%d,qs%d>,stage%d,split%d", t.BM, t.BN, t.MI,
-                  t.WK, c.QS, c.P * l.KR, c.splits);
+    std::snprintf(buf, sizeof buf, "nm_half_tile_kernel<%dx%d,mi%d,ct%d,wk%d,qs%d>,stage%d,split%d", t.BM, t.BN, t.MI,
+                  t.CT, t.WK, c.QS, c.P * l.KR, c.splits);
     return buf;
 }
 

@@ -36,3 +36,14 @@ def test_half_workspace_counts_rows_of_a_off_16_bytes(m, k, n, N, M, V):
     assert L.nmspmm_half_kernel_name(m, weight, 1).startswith(b"nm_half_short_kernel")
     size = L.nmspmm_half_workspace_bytes(m, weight)
     assert size >= 2 * m * n * 4 and size % (m * n * 4) == 0
+
+
+@pytest.mark.parametrize("m,k,n,N,M", [(4096, 4096, 4096, 16, 32), (4096, 4096, 4096, 4, 32), (2048, 4096, 11008, 8, 32),
+                                       (2500, 160, 4608, 16, 32)])
+def test_half_large_tiles_gather_once_for_two_operands(m, k, n, N, M):
+    """Where V is a multiple of 64 a gathered row serves two operands in the
+    largest tiles, and cannot where it is not."""
+    for V, ct in ((32, b",ct1,"), (64, b",ct2,"), (192, b",ct2,"), (96, b",ct1,")):
+        weight = ctypes.pointer(serve._Weight(PTR, nm.NMSPMM_BF16, N, M, V, k, n // (2 * V) * 2 * V))
+        name = serve._library().nmspmm_half_kernel_name(m, weight, 1)
+        assert name.startswith(b"nm_half_tile_kernel<128x256,mi32") and ct in name, (V, name)
