@@ -154,9 +154,12 @@ def nmspmm_half_pack(Bc, idx, n: int, k: int, N: int, M: int, V: int, dtype=None
         dtype = torch.bfloat16 if Bc.dtype == torch.float32 else Bc.dtype
     at = Bc.get_device()
     if packed is None:
-        packed = torch.empty(size, dtype=torch.uint8, device=Bc.device)
+        # from the pool of the stream that writes it: a block of the current
+        # stream's may still be in use by work queued there
+        with torch.cuda.stream(stream):     # (None: the current one)
+            packed = torch.empty(size, dtype=torch.uint8, device=Bc.device)
         if stream is not None:
-            packed.record_stream(stream)
+            packed.record_stream(torch.cuda.current_stream(at))
     elif _workspace(packed, Bc.device, "packed")[1] < size:
         raise ValueError(f"packed has {packed.numel()} bytes, {size} needed")
     weight = HalfWeight(packed, dtype, k, n, N, M, V)
