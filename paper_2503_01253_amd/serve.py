@@ -189,18 +189,23 @@ def nmspmm_half_run(A, weight: HalfWeight, C, alpha: float = 1.0, bias=None, act
     nmspmm_half_workspace_bytes bytes (or None: the library's own)."""
     import torch
     L = _lib or _library()
-    at = weight.at
-    dtype, c_dtype, shape, n = weight.dtype, C.dtype, C.shape, weight.n
-    extra = [x for x in (mul, residual) if x is not None]
     # one expression for what holds in every good call (a call's host time is
     # of the order of a small product's GPU time); _check_half words the rest
-    if not (A.dtype is dtype and (c_dtype is dtype or c_dtype is torch.float32) and A.get_device() == at
-            and C.get_device() == at and len(shape) == 2 and A.shape == (shape[0], weight.k) and shape[1] == n
-            and A.stride(1) == 1 and C.stride(1) == 1
-            and all(x.dtype is c_dtype and x.get_device() == at and x.shape == shape and x.stride(1) == 1 for x in extra)
-            and (bias is None or (bias.dtype is torch.float32 and bias.get_device() == at and bias.shape == (n,)
-                                  and bias.stride(0) == 1))):
-        _check_half(torch, A, weight, C, bias, mul, residual)
+    try:
+        at, dtype, c_dtype, shape, n = weight.at, weight.dtype, C.dtype, C.shape, weight.n
+        good = (A.dtype is dtype and (c_dtype is dtype or c_dtype is torch.float32) and A.get_device() == at
+                and C.get_device() == at and len(shape) == 2 and A.shape == (shape[0], weight.k) and shape[1] == n
+                and A.stride(1) == 1 and C.stride(1) == 1
+                and (mul is None or (mul.dtype is c_dtype and mul.get_device() == at and mul.shape == shape
+                                     and mul.stride(1) == 1))
+                and (residual is None or (residual.dtype is c_dtype and residual.get_device() == at
+                                          and residual.shape == shape and residual.stride(1) == 1))
+                and (bias is None or (bias.dtype is torch.float32 and bias.get_device() == at and bias.shape == (n,)
+                                      and bias.stride(0) == 1)))
+    except AttributeError:      # no tensor, or no handle
+        good = False
+    if not good:
+        _check_half(A, weight, C, bias, mul, residual)
     if act not in HALF_ACTS:
         raise ValueError(f"act must be one of {sorted(HALF_ACTS)}")
     ws, size = (None, 0) if workspace is None else _workspace(workspace, weight.device)
@@ -214,7 +219,10 @@ def nmspmm_half_run(A, weight: HalfWeight, C, alpha: float = 1.0, bias=None, act
     return C
 
 
-def _check_half(torch, A, weight, C, bias, mul, residual):
+def _check_half(A, weight, C, bias, mul, residual):
+    import torch
+    if not isinstance(weight, HalfWeight):
+        raise TypeError("weight must be a HalfWeight")
     dev = weight.device
     _require("A", A, (weight.dtype,), 2, dev)
     _shape("A", A, (A.shape[0], weight.k))
@@ -271,30 +279,45 @@ def nmspmm_kv_append(cache: KvCache, k, v, seq, pos, cos=None, sin=None, q=None,
     negative position, say) are skipped.  Returns q_out."""
     import torch
     L = _lib or _library()
-    at, dtype, shape = cache.at, k.dtype, k.shape
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin go together")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
     if q is not None and q_out is None:
         q_out = q
-    ks, vs = k.stride(), v.stride()
-    # as in nmspmm_half_run: one expression, and _check_append words the rest
-    if not (dtype in _dtypes and v.dtype is dtype and k.get_device() == at and v.get_device() == at
-            and len(shape) == 3 and v.shape == shape and shape[1] == cache.heads and shape[2] == cache.dim
-            and ks[2] == 1 and vs[2] == 1 and all(
-                x.dtype is torch.int32 and x.get_device() == at and x.shape == shape[:1] and x.stride(0) == 1
-                for x in (seq, pos))):
-        _check_append(torch, cache, k, v, seq, pos)
-    angles = (None, None, 0, 0)
-    if cos is not None or sin is not None:
-        if not (cos.dtype is torch.float32 and sin.dtype is torch.float32 and cos.get_device() == at
-                and sin.get_device() == at and cos.dim() == 2 and sin.shape == cos.shape and cos.is_contiguous()
-                and sin.is_contiguous()):
-            _check_angles(torch, cache, cos, sin)
+    angles, queries = (None, None, 0, 0), (None, None, None, None, 0)
+    # as in nmspmm_half_run: one expression, and the _check_ functions word the rest
+    try:
+        at, dtype, shape, ks, vs = cache.at, k.dtype, k.shape, k.stride(), v.stride()
+        good = (dtype in _dtypes and v.dtype is dtype and k.get_device() == at and v.get_device() == at
+                and len(shape) == 3 and v.shape == shape and shape[1] == cache.heads and shape[2] == cache.dim
+                and ks[2] == 1 and vs[2] == 1 and seq.dtype is torch.int32 and pos.dtype is torch.int32
+                and seq.get_device() == at and pos.get_device() == at and seq.shape == shape[:1]
+                and pos.shape == seq.shape and seq.stride(0) == 1 and pos.stride(0) == 1)
+    except AttributeError:
+        good = False
+    if not good:
+        _check_append(cache, k, v, seq, pos)
+    if cos is not None:
+        try:
+            good = (cos.dtype is torch.float32 and sin.dtype is torch.float32 and cos.get_device() == at
+                    and sin.get_device() == at and cos.dim() == 2 and sin.shape == cos.shape and cos.is_contiguous()
+                    and sin.is_contiguous())
+        except AttributeError:
+            good = False
+        if not good:
+            _check_angles(cache, cos, sin)
         rows, half = cos.shape
         angles = (cos.data_ptr(), sin.data_ptr(), rows, 2 * half)
-    queries = (None, None, None, None, 0)
     if q is not None:
-        heads, qs, qos = q.shape[1], q.stride(), q_out.stride()
-        if not (q.dtype is dtype and q_out.dtype is dtype and q.get_device() == at and q_out.get_device() == at
-                and q.shape == (shape[0], heads, cache.dim) and q_out.shape == q.shape and qs[2] == 1 and qos[2] == 1):
+        try:
+            heads, qs, qos = q.shape[1], q.stride(), q_out.stride()
+            good = (q.dtype is dtype and q_out.dtype is dtype and q.get_device() == at and q_out.get_device() == at
+                    and q.shape == (shape[0], heads, cache.dim) and q_out.shape == q.shape and qs[2] == 1
+                    and qos[2] == 1)
+        except (AttributeError, IndexError):
+            good = False
+        if not good:
             _check_queries(cache, k, q, q_out)
         queries = (q.data_ptr(), _Pair(qs[0], qs[1]), q_out.data_ptr(), _Pair(qos[0], qos[1]), heads)
     st = _call(torch, at, L.nmspmm_kv_append, cache._ref, k.data_ptr(), _Pair(ks[0], ks[1]), v.data_ptr(),
@@ -305,7 +328,14 @@ def nmspmm_kv_append(cache: KvCache, k, v, seq, pos, cos=None, sin=None, q=None,
     return q_out
 
 
-def _check_append(torch, cache, k, v, seq, pos):
+def _check_cache(cache):
+    if not isinstance(cache, KvCache):
+        raise TypeError("cache must be a KvCache")
+
+
+def _check_append(cache, k, v, seq, pos):
+    import torch
+    _check_cache(cache)
     _require("k", k, tuple(_dtypes), 3, cache.device)
     _shape("k", k, (k.shape[0], cache.heads, cache.dim))
     _require("v", v, (k.dtype,), 3, cache.device)
@@ -315,7 +345,8 @@ def _check_append(torch, cache, k, v, seq, pos):
         _shape(name, t, k.shape[:1])
 
 
-def _check_angles(torch, cache, cos, sin):
+def _check_angles(cache, cos, sin):
+    import torch
     for name, t in (("cos", cos), ("sin", sin)):
         _require(name, t, (torch.float32,), 2, cache.device)
         _shape(name, t, cos.shape)
@@ -348,13 +379,17 @@ def nmspmm_kv_attend(cache: KvCache, q, lengths, out, scale=None, window: int = 
     bytes."""
     import torch
     L = _lib or _library()
-    at, dtype, shape, qs, outs = cache.at, q.dtype, q.shape, q.stride(), out.stride()
     # as in nmspmm_half_run: one expression, and _check_attend words the rest
-    if not (dtype in _dtypes and out.dtype is dtype and q.get_device() == at and out.get_device() == at
-            and len(shape) == 3 and shape[0] == cache.sequences and shape[2] == cache.dim and out.shape == shape
-            and qs[2] == 1 and outs[2] == 1 and lengths.dtype is torch.int32 and lengths.get_device() == at
-            and lengths.shape == shape[:1] and lengths.stride(0) == 1 and lse is None):
-        _check_attend(torch, cache, q, lengths, out, lse)
+    try:
+        at, dtype, shape, qs, outs = cache.at, q.dtype, q.shape, q.stride(), out.stride()
+        good = (dtype in _dtypes and out.dtype is dtype and q.get_device() == at and out.get_device() == at
+                and len(shape) == 3 and shape[0] == cache.sequences and shape[2] == cache.dim and out.shape == shape
+                and qs[2] == 1 and outs[2] == 1 and lengths.dtype is torch.int32 and lengths.get_device() == at
+                and lengths.shape == shape[:1] and lengths.stride(0) == 1 and lse is None)
+    except AttributeError:
+        good = False
+    if not good:
+        _check_attend(cache, q, lengths, out, lse)
     if max_length is None:
         max_length = cache.table_pages * cache.page_size
     if scale is None:
@@ -368,7 +403,9 @@ def nmspmm_kv_attend(cache: KvCache, q, lengths, out, scale=None, window: int = 
     return out
 
 
-def _check_attend(torch, cache, q, lengths, out, lse):
+def _check_attend(cache, q, lengths, out, lse):
+    import torch
+    _check_cache(cache)
     dev = cache.device
     _require("q", q, tuple(_dtypes), 3, dev)
     _shape("q", q, (cache.sequences, q.shape[1], cache.dim))
