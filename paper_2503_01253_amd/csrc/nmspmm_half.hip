@@ -305,7 +305,9 @@ HalfPlan half_plan(int64_t m, const HalfLayout &l, const nmspmm_half_weight_t &w
     HalfPlan best;
     if (l.MI == 0 || w.k == 0 || w.k >= (int64_t)1 << 21) return best;
     double best_cost = 1e300;
-    if (m <= HS_ROWS && vec && l.S * l.STEP == l.G * w.N && l.windows % l.G == 0) {
+    // (a launch takes fewer than 2^32 threads)
+    if (m <= HS_ROWS && vec && l.S * l.STEP == l.G * w.N && l.windows % l.G == 0 &&
+        w.n / l.MI < ((int64_t)1 << 32) / HS_NT) {
         // the largest chunk of A that a slot holds, then the chunks made even
         best.wide = w.n / l.MI <= 256;
         const int slot = best.wide ? HS_SLOT_WIDE : HS_SLOT;

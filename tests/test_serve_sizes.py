@@ -47,3 +47,14 @@ def test_half_large_tiles_gather_once_for_two_operands(m, k, n, N, M):
         weight = ctypes.pointer(serve._Weight(PTR, nm.NMSPMM_BF16, N, M, V, k, n // (2 * V) * 2 * V))
         name = serve._library().nmspmm_half_kernel_name(m, weight, 1)
         assert name.startswith(b"nm_half_tile_kernel<128x256,mi32") and ct in name, (V, name)
+
+
+@pytest.mark.parametrize("n,V,short", [(2 ** 28 - 2 ** 20, 2 ** 20, True), (2 ** 28, 2 ** 20, False),
+                                       (2 ** 30, 2 ** 28, False), (2 ** 27, 2 ** 20 + 16, False)])
+def test_half_few_rows_within_a_launch(n, V, short):
+    """A launch takes fewer than 2^32 threads: weights of 2^28 columns (2^27 in
+    operands of 16) are not the few-row kernel's, 512 threads an operand."""
+    if V % 32:
+        n = (n // V + 1) * V
+    weight = ctypes.pointer(serve._Weight(PTR, nm.NMSPMM_BF16, 4, 32, V, 256, n))
+    assert serve._library().nmspmm_half_kernel_name(1, weight, 1).startswith(b"nm_half_short_kernel") == short
