@@ -148,9 +148,10 @@ __global__ __launch_bounds__(128) void nm_half_pack_kernel(PackArgs p)
     const S *Bc = static_cast<const S *>(p.Bc);
     T *vals = static_cast<T *>(p.vals);
     // a lane's eight rows, of every operand of the unit in the block's tiles
-    for (int e = i; e < p.V / MI * p.l.S * 64; e += 128) {
-        const int lane = e % 64, s = e / 64 % p.l.S;
-        const int64_t tile = block * (p.V / MI) + e / 64 / p.l.S, col = tile * MI + lane % MI;
+    const int lane = i % 64;
+    for (int o = i / 64; o < p.V / MI * p.l.S; o += 2) {
+        const int s = o % p.l.S;
+        const int64_t tile = block * (p.V / MI) + o / p.l.S, col = tile * MI + lane % MI;
         T *dst = vals + ((tile * p.l.steps + unit * p.l.S + s) * 64 + lane) * 8;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
