@@ -251,6 +251,8 @@ class KvCache:
         _require("v_pages", v_pages, (k_pages.dtype,), 4, k_pages.device)
         _shape("v_pages", v_pages, k_pages.shape)
         _require("table", table, (torch.int32,), 2, k_pages.device)
+        if max(k_pages.shape[1:]) > 2 ** 31 - 1:
+            raise ValueError(f"k_pages has shape {tuple(k_pages.shape)}: a page's sizes are 32-bit")
         self.k_pages, self.v_pages, self.table = k_pages, v_pages, table
         self.device, self.dtype, self.at = k_pages.device, k_pages.dtype, k_pages.get_device()
         self.pages, self.page_size, self.heads, self.dim = k_pages.shape

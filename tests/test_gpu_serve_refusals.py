@@ -79,3 +79,12 @@ def test_attend(cache):
         for x in (good[name][:-1], good[name][None], torch.cat((good[name], good[name]), -1)[..., ::2]):
             with pytest.raises(ValueError):
                 nm.nmspmm_kv_attend(cache, **{**good, name: x})
+
+
+def test_cache_sizes_beyond_32_bits():
+    """The C structure holds a page's sizes in 32 bits: 2^32 + 16 would be 16."""
+    table = new(1, 1, dtype=torch.int32)
+    for shape in ((1, 2 ** 32 + 16, 1, 64), (1, 16, 2 ** 32 + 2, 64)):
+        far = new(1, 1, 1, 64).expand(shape)
+        with pytest.raises(ValueError, match="32-bit"):
+            nm.nmspmm_kv_cache(far, far, table)
