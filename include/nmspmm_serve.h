@@ -93,7 +93,7 @@ NMSPMM_API int64_t nmspmm_half_workspace_bytes(int64_t m, const nmspmm_half_weig
  * A weight of which some whole windows, 128 columns of A at most, come to a
  * multiple of 8 columns and to 64 kept rows at most (128 where V is no multiple of
  * 32) runs on the matrix instructions where V is a multiple of 16, k below 2^21
- * and lda too; any other, on a kernel of 4 to 6 TFLOP/s.
+ * and lda too; any other, on a kernel of 3 to 6 TFLOP/s.
  * m == 0 or n == 0 returns NMSPMM_OK without a launch; with k == 0 the sum is
  * zero.  Errors: NMSPMM_ERR_INVALID_ARG (bad shape, type or activation, a row
  * stride below the row's length, null pointer with non-empty data),

@@ -102,6 +102,7 @@ __global__ __launch_bounds__(256) void nm_half_pack_raw_kernel(const S *Bc, cons
 // of a class goes to group r, and what a class has beyond the number of groups
 // fills the places other classes leave, which are those of the last groups.
 // (In the order of the columns a read took 2.2 cycles more than it needs.)
+// 4096 x 11008 at 8:32 from fp32 46 us, 68 MB: once a weight.
 template <class T, class S>
 __global__ __launch_bounds__(128) void nm_half_pack_kernel(PackArgs p)
 {
@@ -184,7 +185,7 @@ constexpr int HG_ROWS = 8;
 
 // Any shape: a thread owns one column and HG_ROWS rows of C and walks the
 // compressed rows of either layout; bound by the loads of A, one value per
-// multiply-add: 4 to 6 TFLOP/s (4096^3 at 16:32 11.6 ms).
+// multiply-add: 3 to 6 TFLOP/s (4096^3 at 16:32 11.6 ms).
 template <class T, class O>
 __global__ __launch_bounds__(256) void nm_half_general_kernel(GeneralArgs p)
 {

@@ -12,7 +12,7 @@
 //         start four banks apart).  The tiled kernel's transposed reads need
 //         A_s k-major, 32 rows wide whatever m is, and a transposition first.
 // The waves' sums meet in LDS and are added in their order; one output a
-// thread goes through the epilogue.  1 x 8192 x 8192 at 4:32 takes 7.0 us (2.4
+// thread goes through the epilogue.  1 x 8192 x 8192 at 4:32 takes 7.2 us (2.3
 // TB/s of weight), 1 x 4096 x 11008 at 8:32 10.3 with its launch; the tiled
 // kernel 16.5 on the former.  A weight whose operands hold padding rows
 // (which would need zeros in A_s) takes the tiled kernel.

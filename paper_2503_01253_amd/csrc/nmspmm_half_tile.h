@@ -29,11 +29,12 @@
 // lane forms its address with four instructions.  The WK waves of a tile share
 // out the units of every stage and are joined through LDS at the end.
 //
-// 4096^3 at 16:32, V = 32, takes 91 us in the kernel (750 TFLOP/s useful),
-// 2048 x 4096 x 11008 at 8:32 96: at 2.0 GHz, the power limit, matrix
-// instructions 33 % busy, LDS 35 %.  By what is left out of a copy, the times
-// add up: instructions, gathers and barriers 57 us, B 14, LDS writes of A 9, its loads 9,
-// epilogue 15.
+// 4096^3 at 16:32 takes 93-95 us in the kernel with V = 32 (730 TFLOP/s useful),
+// 88 with V = 64 and two operands a gather, 2048 x 4096 x 11008 at 8:32 97: at 2.2
+// GHz, matrix instructions 32 % busy, LDS 34 % (24 with V = 64).  Little overlaps:
+// in a row of calls (101 us, V = 32) a copy takes 89 us without A's loads, 75
+// without its LDS writes too, 92 without B, 42 without gathers and matrix
+// instructions, 18 without all of them.
 #ifndef NMSPMM_HALF_TILE_H
 #define NMSPMM_HALF_TILE_H
 

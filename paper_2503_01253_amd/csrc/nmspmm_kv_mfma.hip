@@ -27,8 +27,8 @@
 // v_mfma_f32_16x16x4_f32 219, 32 ragged sequences of 4 heads of 256 82, 88 and 99.)
 // The next tokens' K is on its way while the weights form, the next V while
 // it is multiplied.  The waves are joined in LDS.  Bound by HBM: 128 x 8192
-// positions, 32 heads on 8 of 128, 771 us (5.6 TB/s), one sequence of 131071
-// 114 us (4.7 TB/s).
+// positions, 32 heads on 8 of 128, 781-787 us (5.5 TB/s), one sequence of 131071
+// 113-115 us (4.7 TB/s).
 #include "nmspmm_kv.h"
 
 namespace nmspmm {
