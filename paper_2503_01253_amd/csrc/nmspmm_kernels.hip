@@ -12,6 +12,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <condition_variable>
 #include <cstdint>
 #include <cstdio>
 #include <cstdlib>
@@ -1251,7 +1252,10 @@ nmspmm_status_t check_run_args(const float *A, const float *Bc, const uint8_t *i
 // (and again, larger, when a call needs more) and kept for the next calls on
 // that stream.  Each call makes its stream wait for the event the buffer's
 // previous user recorded after its kernels, and records it again after its
-// own.  Calls on one stream are ordered anyway; the wait orders the first
+// own.  Calls on one stream are ordered anyway, each with its kernels in one
+// run: a host thread that finds the buffer of its stream with another thread's
+// call waits (host time only, a call's launches), since kernels of two calls in
+// turn would overwrite each other's contents.  The wait for the event orders the first
 // call on a stream whose handle reuses that of a destroyed one (HIP hands a
 // new stream the last destroyed stream's handle) after the destroyed
 // stream's last kernels.  The pair costs about 1.4 us of host time per call
@@ -1270,11 +1274,12 @@ struct WsEntry {
     size_t bytes = 0;
     hipEvent_t done = nullptr;
     uint64_t used = 0;   // call counter of the last use (for the oldest entry)
-    int busy = 0;        // calls between ws_acquire and ws_done (never dropped then)
+    int busy = 0;        // 1 from ws_acquire to ws_done (not dropped or shared then)
 };
 WsEntry g_ws[kWsEntries];
 uint64_t g_ws_calls = 0;
 std::mutex g_ws_mu;
+std::condition_variable g_ws_free;      // an entry's call is over
 
 // Release an entry's buffer and event after its last kernels.
 void ws_drop(WsEntry &e)
@@ -1294,17 +1299,19 @@ void *ws_acquire(hipStream_t stream, size_t need, int *slot)
         (void)hipGetLastError();
         return nullptr;
     }
-    std::lock_guard<std::mutex> lock(g_ws_mu);
-    int hit = -1, oldest = -1;
-    for (int i = 0; i < kWsEntries; ++i) {
-        if (g_ws[i].buf && g_ws[i].dev == dev && g_ws[i].stream == stream) hit = i;
-        if (g_ws[i].buf && g_ws[i].busy == 0 && (oldest < 0 || g_ws[i].used < g_ws[oldest].used)) oldest = i;
+    std::unique_lock<std::mutex> lock(g_ws_mu);
+    int hit, oldest;
+    for (;;) {
+        hit = oldest = -1;
+        for (int i = 0; i < kWsEntries; ++i) {
+            if (g_ws[i].buf && g_ws[i].dev == dev && g_ws[i].stream == stream) hit = i;
+            if (g_ws[i].buf && g_ws[i].busy == 0 && (oldest < 0 || g_ws[i].used < g_ws[oldest].used)) oldest = i;
+        }
+        if (hit < 0 || g_ws[hit].busy == 0) break;
+        g_ws_free.wait(lock);
     }
     int i = hit;
-    if (i >= 0 && g_ws[i].bytes < need) {
-        if (g_ws[i].busy > 0) return nullptr;
-        ws_drop(g_ws[i]);   // grow: the old buffer after its last use
-    }
+    if (i >= 0 && g_ws[i].bytes < need) ws_drop(g_ws[i]);   // grow: the old buffer after its last use
     if (i < 0) {
         for (int j = 0; j < kWsEntries && i < 0; ++j)
             if (!g_ws[j].buf) i = j;
@@ -1346,8 +1353,10 @@ void *ws_acquire(hipStream_t stream, size_t need, int *slot)
 hipError_t ws_done(int slot, hipStream_t stream)
 {
     std::lock_guard<std::mutex> lock(g_ws_mu);
+    const hipError_t e = hipEventRecord(g_ws[slot].done, stream);
     --g_ws[slot].busy;
-    return hipEventRecord(g_ws[slot].done, stream);
+    g_ws_free.notify_all();
+    return e;
 }
 
 bool capturing(hipStream_t stream)
