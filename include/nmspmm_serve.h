@@ -56,7 +56,7 @@ NMSPMM_API int64_t nmspmm_half_bytes(int64_t k, int64_t n, int N, int M, int V);
  * weight->dtype (ties to even).  An offset >= M is clamped to M-1, as
  * nmspmm_run does.  Errors: NMSPMM_ERR_INVALID_ARG (bad shape or type, null
  * pointer with non-empty data), NMSPMM_ERR_UNSUPPORTED (misaligned pointer,
- * sizes beyond int64), NMSPMM_ERR_HIP. */
+ * sizes beyond int64, n of 2^31 or more), NMSPMM_ERR_HIP. */
 NMSPMM_API nmspmm_status_t nmspmm_half_pack(const void *Bc, nmspmm_dtype_t bc_dtype, const uint8_t *idx,
                                  const nmspmm_half_weight_t *weight, hipStream_t stream);
 
@@ -97,8 +97,8 @@ NMSPMM_API int64_t nmspmm_half_workspace_bytes(int64_t m, const nmspmm_half_weig
  * m == 0 or n == 0 returns NMSPMM_OK without a launch; with k == 0 the sum is
  * zero.  Errors: NMSPMM_ERR_INVALID_ARG (bad shape, type or activation, a row
  * stride below the row's length, null pointer with non-empty data),
- * NMSPMM_ERR_UNSUPPORTED (misaligned pointer, sizes beyond int64),
- * NMSPMM_ERR_HIP. */
+ * NMSPMM_ERR_UNSUPPORTED (misaligned pointer, sizes beyond int64, n of 2^31 or
+ * more), NMSPMM_ERR_HIP. */
 NMSPMM_API nmspmm_status_t nmspmm_half_run(const void *A, int64_t lda, const nmspmm_half_weight_t *weight, void *C,
                                 int64_t ldc, nmspmm_dtype_t c_dtype, int64_t m, float alpha, const float *bias,
                                 nmspmm_half_act_t act, const void *mul, int64_t ld_mul, const void *residual,
@@ -151,7 +151,9 @@ typedef struct {
  * by value, one of the two.  tokens == 0 returns NMSPMM_OK without a launch.  Errors:
  * NMSPMM_ERR_INVALID_ARG (negative size, bad type, odd rot or rot > dim, null
  * pointer with non-empty data), NMSPMM_ERR_UNSUPPORTED (misaligned pointer,
- * dim > 512, more than 2^31 - 1 tokens, heads or positions), NMSPMM_ERR_HIP. */
+ * dim > 512, more than 2^31 - 1 positions, 2^24 tokens or more, more than 2^24 -
+ * 256 pairs of dimensions a token, keys, values and queries together),
+ * NMSPMM_ERR_HIP. */
 NMSPMM_API nmspmm_status_t nmspmm_kv_append(const nmspmm_kv_cache_t *cache, const void *k_new, const int64_t *k_stride,
                                  const void *v_new, const int64_t *v_stride, nmspmm_dtype_t dtype,
                                  int64_t tokens, const int32_t *seq, const int32_t *pos, const float *cos,

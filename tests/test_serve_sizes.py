@@ -58,3 +58,23 @@ def test_half_few_rows_within_a_launch(n, V, short):
         n = (n // V + 1) * V
     weight = ctypes.pointer(serve._Weight(PTR, nm.NMSPMM_BF16, 4, 32, V, 256, n))
     assert serve._library().nmspmm_half_kernel_name(1, weight, 1).startswith(b"nm_half_short_kernel") == short
+
+
+def test_sizes_that_the_header_names():
+    """The first sizes that are refused, before anything is read."""
+    L = serve._library()
+    P2 = (ctypes.c_int64 * 2)(128, 64)
+    strides = (ctypes.c_int64 * 3)(2048, 128, 64)
+
+    def append(tokens=1, q_heads=0, positions=0):
+        cache = ctypes.pointer(serve._Cache(PTR, PTR, strides, strides, 4, PTR, 4, 1, 4, 16, 2, 64, nm.NMSPMM_BF16))
+        return L.nmspmm_kv_append(cache, PTR, P2, PTR, P2, nm.NMSPMM_BF16, tokens, PTR, PTR, None, None, positions, 0, 0,
+                                  PTR, P2, PTR, P2, q_heads, None)
+
+    assert append(tokens=2 ** 24) == nm.NMSPMM_ERR_UNSUPPORTED
+    assert append(positions=2 ** 31) == nm.NMSPMM_ERR_UNSUPPORTED
+    assert append(q_heads=(2 ** 24 - 256) // 32 - 4 + 1) == nm.NMSPMM_ERR_UNSUPPORTED
+    wide = ctypes.pointer(serve._Weight(PTR, nm.NMSPMM_BF16, 4, 32, 32, 32, 2 ** 31))
+    assert L.nmspmm_half_pack(PTR, nm.NMSPMM_F32, PTR, wide, None) == nm.NMSPMM_ERR_UNSUPPORTED
+    assert L.nmspmm_half_run(PTR, 32, wide, PTR, 2 ** 31, nm.NMSPMM_BF16, 1, 1.0, None, 0, None, 0, None, 0, None, 0,
+                             None) == nm.NMSPMM_ERR_UNSUPPORTED
