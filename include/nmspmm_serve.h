@@ -161,6 +161,23 @@ NMSPMM_API nmspmm_status_t nmspmm_kv_append(const nmspmm_kv_cache_t *cache, cons
                                  const int64_t *q_stride, void *q_out, const int64_t *q_out_stride,
                                  int64_t q_heads, hipStream_t stream);
 
+/* nmspmm_kv_append with a norm of every head before the rotation, in the same
+ * pass: a query (with q_norm) or key (with k_norm) x becomes
+ *   x[d] * weight[d] / sqrt(mean(x^2) + eps)     over its dim dimensions
+ *   q_norm, k_norm   dim fp32 weights, or NULL: no norm of the queries or keys
+ * Norm (its sum fp64) and rotation are fp32, and a value is rounded once, after
+ * both.  All else as in nmspmm_kv_append, but for the sizes it refuses: 2^24 tokens or
+ * more, 2^17 heads or more, keys, values and queries together.  Errors: as there, and
+ * NMSPMM_ERR_INVALID_ARG for an eps that is negative or NaN,
+ * NMSPMM_ERR_UNSUPPORTED for misaligned weights. */
+NMSPMM_API nmspmm_status_t nmspmm_kv_append_norm(const nmspmm_kv_cache_t *cache, const void *k_new,
+                                      const int64_t *k_stride, const void *v_new, const int64_t *v_stride,
+                                      nmspmm_dtype_t dtype, int64_t tokens, const int32_t *seq, const int32_t *pos,
+                                      const float *cos, const float *sin, int64_t positions, int rot, int interleaved,
+                                      const float *q_norm, const float *k_norm, float eps, const void *q,
+                                      const int64_t *q_stride, void *q_out, const int64_t *q_out_stride,
+                                      int64_t q_heads, hipStream_t stream);
+
 /* Bytes of workspace with which nmspmm_kv_attend splits the sequences of this
  * cache: 0 where it does not, -1 for bad sizes.  Host only. */
 NMSPMM_API int64_t nmspmm_kv_attend_workspace_bytes(const nmspmm_kv_cache_t *cache, int64_t q_heads,

@@ -15,5 +15,10 @@ from .binding import (  # noqa: F401
 from .serve import (  # noqa: F401
     HALF_ACTS, NMSPMM_BF16, NMSPMM_F16, NMSPMM_F32, SERVE_EXPORTS, HalfWeight, KvCache,
     nmspmm_half_bytes, nmspmm_half_kernel_name, nmspmm_half_pack, nmspmm_half_run, nmspmm_half_workspace_bytes,
-    nmspmm_kv_append, nmspmm_kv_attend, nmspmm_kv_attend_workspace_bytes, nmspmm_kv_cache,
+    nmspmm_kv_append, nmspmm_kv_append_norm, nmspmm_kv_attend, nmspmm_kv_attend_workspace_bytes, nmspmm_kv_cache,
+)
+from .mx4 import (  # noqa: F401
+    MX4_EXPORTS, Kv4Cache, Mx4Weight, nmspmm_kv4_append, nmspmm_kv4_attend, nmspmm_kv4_attend_workspace_bytes,
+    nmspmm_kv4_cache, nmspmm_kv4_page_bytes, nmspmm_kv4_read, nmspmm_mx4_bytes, nmspmm_mx4_kernel_name,
+    nmspmm_mx4_pack, nmspmm_mx4_quantize, nmspmm_mx4_run, nmspmm_mx4_workspace_bytes,
 )

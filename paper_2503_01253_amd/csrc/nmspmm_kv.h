@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "nmspmm_dtype.h"
 #include "nmspmm_serve.h"
@@ -51,12 +52,42 @@ __device__ __forceinline__ Place place_of(const Pages &c, const int32_t *row, in
     return {page, pos - (int32_t)(at * c.size.d), page >= 0 && page < c.pages};
 }
 
+// (a, b) turned by the angle of cos c and sin s.  Spelled with fused
+// multiply-adds whose fp32 results are kept (fp16's rounding is not fused into
+// them), so that every kernel rounds alike.
+__device__ __forceinline__ void turn_pair(float &a, float &b, float c, float s)
+{
+    float x = fmaf(a, c, -(b * s)), y = fmaf(a, s, b * c);
+#ifdef __HIP_DEVICE_COMPILE__
+    asm("" : "+v"(x), "+v"(y));
+#endif
+    a = x;
+    b = y;
+}
+
 constexpr float NEG_INF = -__builtin_inff();
 
 // The reference a running maximum stands for: scores are taken relative to
 // it, and where nothing has been seen (minus infinity) relative to 0, so that
 // no difference of two infinities arises.
 __device__ __forceinline__ float softmax_ref(float m) { return m == NEG_INF ? 0.f : m; }
+
+// The sum of x over the LPT lanes of a team, in every one of them.
+template <int LPT>
+__device__ __forceinline__ float lanes_sum(float x)
+{
+    auto dpp = [](float v, auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value,
+                                                                     0xf, 0xf, false));
+    };
+    x += dpp(x, std::integral_constant<int, 0xb1>{});                          // lane ^ 1
+    x += dpp(x, std::integral_constant<int, 0x4e>{});                          // lane ^ 2
+    if constexpr (LPT >= 8) x += dpp(x, std::integral_constant<int, 0x141>{});  // the other four of eight
+    if constexpr (LPT >= 16) x += dpp(x, std::integral_constant<int, 0x140>{}); // the other eight of sixteen
+    if constexpr (LPT >= 32) x += __shfl_xor(x, 16);
+    if constexpr (LPT >= 64) x += __shfl_xor(x, 32);
+    return x;
+}
 
 struct AttendArgs {
     Pages c;

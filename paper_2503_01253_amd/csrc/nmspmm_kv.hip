@@ -5,63 +5,11 @@
 #include <cstdint>
 
 #include "nmspmm_kv.h"
+#include "nmspmm_kv_host.h"
 #include "nmspmm_workspace.h"
 
 namespace nmspmm {
 namespace {
-
-bool aligned_to(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-constexpr int64_t INT31 = 0x7fffffff;
-constexpr int KV_MAX_DIM = 512;
-constexpr int64_t KV_MAX_LENGTH = INT31 - 4096;     // the kernels step a few hundred positions past the last
-
-nmspmm_status_t check_cache(const nmspmm_kv_cache_t *c)
-{
-    if (!c || c->pages < 0 || c->sequences < 0 || c->table_pages < 0 || c->page_size < 1 || c->heads < 1 ||
-        c->dim < 1 || !dtype_ok(c->dtype))
-        return NMSPMM_ERR_INVALID_ARG;
-    if (c->dim > KV_MAX_DIM || c->sequences > INT31 || c->pages > INT31 || c->table_pages > INT31)
-        return NMSPMM_ERR_UNSUPPORTED;
-    return NMSPMM_OK;
-}
-
-nmspmm_status_t check_cache_pointers(const nmspmm_kv_cache_t *c)
-{
-    if (c->pages > 0 && (!c->k_pages || !c->v_pages)) return NMSPMM_ERR_INVALID_ARG;
-    if (c->sequences > 0 && c->table_pages > 0 && !c->table) return NMSPMM_ERR_INVALID_ARG;
-    const int es = dtype_bytes(c->dtype);
-    if (!aligned_to(c->k_pages, es) || !aligned_to(c->v_pages, es) || !aligned_to(c->table, 4))
-        return NMSPMM_ERR_UNSUPPORTED;
-    return NMSPMM_OK;
-}
-
-Pages device_view(const nmspmm_kv_cache_t *c)
-{
-    Pages p;
-    p.table = c->table;
-    p.table_stride = c->table_stride;
-    p.pages = c->pages;
-    for (int i = 0; i < 3; ++i) {
-        p.ks[i] = c->k_stride[i];
-        p.vs[i] = c->v_stride[i];
-    }
-    p.size = fast_div((uint32_t)c->page_size);
-    return p;
-}
-
-// Positions that the table can name, at most 2^31 - 1.
-int64_t table_positions(const nmspmm_kv_cache_t *c) { return std::min(INT31, c->table_pages * c->page_size); }
-
-// Whether rows of `dim` elements of `bytes` bytes at these strides all start
-// on 16 bytes and hold whole 16-byte pieces.
-bool rows_aligned(const void *p, const int64_t *stride, int count, int dim, int bytes)
-{
-    if (!aligned_to(p, 16) || dim * bytes % 16) return false;
-    for (int i = 0; i < count; ++i)
-        if (stride[i] * bytes % 16) return false;
-    return true;
-}
 
 // ---- nmspmm_kv_append ------------------------------------------------------
 
@@ -77,19 +25,6 @@ struct AppendArgs {
 };
 
 constexpr int AP_NT = 256;
-
-// (a, b) turned by the angle of cos c and sin s.  Spelled with fused
-// multiply-adds whose fp32 results are kept (fp16's rounding is not fused into
-// them), so that every kernel rounds alike.
-__device__ __forceinline__ void turn_pair(float &a, float &b, float c, float s)
-{
-    float x = fmaf(a, c, -(b * s)), y = fmaf(a, s, b * c);
-#ifdef __HIP_DEVICE_COMPILE__
-    asm("" : "+v"(x), "+v"(y));
-#endif
-    a = x;
-    b = y;
-}
 
 // Every (token, row, dimension pair) by one thread: a row is a key, a value
 // or a query head; a pair is two dimensions that turn together, or (beyond
@@ -211,22 +146,6 @@ hipError_t launch_append(const AppendArgs &p, nmspmm_dtype_t cache, bool vec, hi
 // ---- nmspmm_kv_attend ------------------------------------------------------
 
 constexpr int AT_NW = 4, AT_NT = 64 * AT_NW;
-
-template <int LPT>
-__device__ __forceinline__ float lanes_sum(float x)
-{
-    auto dpp = [](float v, auto ctrl) {
-        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value,
-                                                                     0xf, 0xf, false));
-    };
-    x += dpp(x, std::integral_constant<int, 0xb1>{});                          // lane ^ 1
-    x += dpp(x, std::integral_constant<int, 0x4e>{});                          // lane ^ 2
-    if constexpr (LPT >= 8) x += dpp(x, std::integral_constant<int, 0x141>{});  // the other four of eight
-    if constexpr (LPT >= 16) x += dpp(x, std::integral_constant<int, 0x140>{}); // the other eight of sixteen
-    if constexpr (LPT >= 32) x += __shfl_xor(x, 16);
-    if constexpr (LPT >= 64) x += __shfl_xor(x, 32);
-    return x;
-}
 
 // The attention of GT query heads that share one cache head, over one chunk
 // of a sequence, on the vector ALU: LPT lanes hold a token's row, EPL
@@ -439,6 +358,8 @@ void launch_join_of(const AttendArgs &p, int64_t rows, hipStream_t stream)
         hipLaunchKernelGGL((nm_attend_join_kernel<512, JN_SPLITS, DL, DV>), dim3((unsigned)rows), dim3(512), 0, stream, p);
 }
 
+}  // namespace
+
 // Four dimensions a thread where they come in fours.
 void launch_join(const AttendArgs &p, int64_t rows, hipStream_t stream)
 {
@@ -447,15 +368,6 @@ void launch_join(const AttendArgs &p, int64_t rows, hipStream_t stream)
     else if (p.dim % 4 == 0) launch_join_of<128, 4>(p, rows, stream);
     else launch_join_of<512, 1>(p, rows, stream);
 }
-
-// How the work is cut: query heads a workgroup takes together, workgroups
-// along a sequence and the positions of each.
-struct AttendPlan {
-    int GT, gtiles, splits, chunk;
-    int64_t groups;             // workgroups
-    int64_t rows;               // sequences x query heads
-    int64_t ml_bytes, bytes;    // workspace
-};
 
 AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window, bool mfma,
                        bool split)
@@ -487,6 +399,8 @@ AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_
     }
     return a;
 }
+
+namespace {
 
 // Whether the matrix-core kernel takes the call: a bf16 cache, or fp16 queries
 // over an fp16 cache (whose range would not hold the parts of others), rows of
@@ -525,6 +439,8 @@ void launch_attend(const AttendArgs &p, bool vec, int GT, unsigned groups, hipSt
     else launch_attend_heads<T, 64, EPL, true>(p, GT, groups, stream);
 }
 
+}  // namespace
+
 nmspmm_status_t check_attend_sizes(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window)
 {
     const nmspmm_status_t st = check_cache(c);
@@ -536,7 +452,6 @@ nmspmm_status_t check_attend_sizes(const nmspmm_kv_cache_t *c, int64_t q_heads, 
     return NMSPMM_OK;
 }
 
-}  // namespace
 }  // namespace nmspmm
 
 using namespace nmspmm;

@@ -18,7 +18,8 @@ HALF_ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 SERVE_EXPORTS = (
     "nmspmm_half_bytes", "nmspmm_half_pack", "nmspmm_half_workspace_bytes", "nmspmm_half_run",
-    "nmspmm_half_kernel_name", "nmspmm_kv_append", "nmspmm_kv_attend_workspace_bytes", "nmspmm_kv_attend",
+    "nmspmm_half_kernel_name", "nmspmm_kv_append", "nmspmm_kv_append_norm", "nmspmm_kv_attend_workspace_bytes",
+    "nmspmm_kv_attend",
 )
 
 
@@ -69,6 +70,8 @@ def declare(L):
     L.nmspmm_half_run.restype = I
     L.nmspmm_kv_append.argtypes = [C, P, S, P, S, I, I64, P, P, P, P, I64, I, I, P, S, P, S, I64, P]
     L.nmspmm_kv_append.restype = I
+    L.nmspmm_kv_append_norm.argtypes = [C, P, S, P, S, I, I64, P, P, P, P, I64, I, I, P, P, F, P, S, P, S, I64, P]
+    L.nmspmm_kv_append_norm.restype = I
     L.nmspmm_kv_attend_workspace_bytes.argtypes = [C, I64, I64, I64]
     L.nmspmm_kv_attend_workspace_bytes.restype = I64
     L.nmspmm_kv_attend.argtypes = [C, P, S, I, I64, P, I64, I64, F, P, S, P, P, Z, P]
@@ -330,14 +333,90 @@ def nmspmm_kv_append(cache: KvCache, k, v, seq, pos, cos=None, sin=None, q=None,
     return q_out
 
 
-def _check_cache(cache):
-    if not isinstance(cache, KvCache):
-        raise TypeError("cache must be a KvCache")
+def nmspmm_kv_append_norm(cache: KvCache, k, v, seq, pos, cos=None, sin=None, q=None, q_out=None, interleaved=False,
+                          q_norm=None, k_norm=None, eps: float = 1e-6, stream=None):
+    """nmspmm_kv_append with a norm of every head before the rotation: with
+    q_norm and k_norm (dim contiguous fp32 weights, either may be None) a query
+    or key x becomes x * weight / sqrt(mean(x^2) + eps).  All else as there."""
+    L = _lib or _library()
+    return _append_norm("nmspmm_kv_append_norm", L.nmspmm_kv_append_norm, KvCache, cache, k, v, seq, pos, cos, sin, q,
+                        q_out, interleaved, q_norm, k_norm, eps, stream)
 
 
-def _check_append(cache, k, v, seq, pos):
+def _append_norm(name, call, kind, cache, k, v, seq, pos, cos, sin, q, q_out, interleaved, q_norm, k_norm, eps, stream):
+    """What the appends with norms share; ``kind``: the cache's class."""
     import torch
-    _check_cache(cache)
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin go together")
+    if q is None and q_out is not None:
+        raise ValueError("q_out without q")
+    if q is not None and q_out is None:
+        q_out = q
+    angles, queries = (None, None, 0, 0), (None, None, None, None, 0)
+    # as in nmspmm_half_run: one expression each, and the _check_ functions word the rest
+    try:
+        at, dtype, shape, ks, vs = cache.at, k.dtype, k.shape, k.stride(), v.stride()
+        good = (type(cache) is kind and dtype in _dtypes and v.dtype is dtype and k.get_device() == at
+                and v.get_device() == at and len(shape) == 3 and v.shape == shape and shape[1] == cache.heads
+                and shape[2] == cache.dim and ks[2] == 1 and vs[2] == 1 and seq.dtype is torch.int32
+                and pos.dtype is torch.int32 and seq.get_device() == at and pos.get_device() == at
+                and seq.shape == shape[:1] and pos.shape == seq.shape and seq.stride(0) == 1 and pos.stride(0) == 1)
+    except AttributeError:
+        good = False
+    if not good:
+        _check_append(cache, k, v, seq, pos, kind)
+    if cos is not None:
+        try:
+            good = (cos.dtype is torch.float32 and sin.dtype is torch.float32 and cos.get_device() == at
+                    and sin.get_device() == at and cos.dim() == 2 and sin.shape == cos.shape and cos.is_contiguous()
+                    and sin.is_contiguous())
+        except AttributeError:
+            good = False
+        if not good:
+            _check_angles(cache, cos, sin)
+        rows, half = cos.shape
+        angles = (cos.data_ptr(), sin.data_ptr(), rows, 2 * half)
+    if q is not None:
+        try:
+            heads, qs, qos = q.shape[1], q.stride(), q_out.stride()
+            good = (q.dtype is dtype and q_out.dtype is dtype and q.get_device() == at and q_out.get_device() == at
+                    and q.shape == (shape[0], heads, cache.dim) and q_out.shape == q.shape and qs[2] == 1
+                    and qos[2] == 1)
+        except (AttributeError, IndexError):
+            good = False
+        if not good:
+            _check_queries(cache, k, q, q_out)
+        queries = (q.data_ptr(), _Pair(qs[0], qs[1]), q_out.data_ptr(), _Pair(qos[0], qos[1]), heads)
+    norms = []
+    for word, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+        if w is None:
+            norms.append(None)
+            continue
+        try:
+            good = (w.dtype is torch.float32 and w.get_device() == at and w.shape == (cache.dim,) and w.stride(0) == 1)
+        except AttributeError:
+            good = False
+        if not good:
+            _require(word, w, (torch.float32,), 1, cache.device)
+            _shape(word, w, (cache.dim,))
+        norms.append(w.data_ptr())
+    st = _call(torch, at, call, cache._ref, k.data_ptr(), _Pair(ks[0], ks[1]), v.data_ptr(), _Pair(vs[0], vs[1]),
+               _dtypes[dtype], shape[0], seq.data_ptr(), pos.data_ptr(), *angles, interleaved, *norms, eps, *queries,
+               _raw_stream(torch, at, stream))
+    if st:
+        _check(name, st)
+    return q_out
+
+
+def _check_cache(cache, kind=None):
+    kind = kind or KvCache
+    if not isinstance(cache, kind):
+        raise TypeError(f"cache must be a {kind.__name__}")
+
+
+def _check_append(cache, k, v, seq, pos, kind=None):
+    import torch
+    _check_cache(cache, kind)
     _require("k", k, tuple(_dtypes), 3, cache.device)
     _shape("k", k, (k.shape[0], cache.heads, cache.dim))
     _require("v", v, (k.dtype,), 3, cache.device)
@@ -405,9 +484,9 @@ def nmspmm_kv_attend(cache: KvCache, q, lengths, out, scale=None, window: int = 
     return out
 
 
-def _check_attend(cache, q, lengths, out, lse):
+def _check_attend(cache, q, lengths, out, lse, kind=None):
     import torch
-    _check_cache(cache)
+    _check_cache(cache, kind)
     dev = cache.device
     _require("q", q, tuple(_dtypes), 3, dev)
     _shape("q", q, (cache.sequences, q.shape[1], cache.dim))
