@@ -10,6 +10,7 @@
 #include "nmspmm_internal.h"
 #include "nmspmm_fp4.h"
 #include "nmspmm_mx4.h"
+#include "nmspmm_mx4_tile.h"
 #include "nmspmm_workspace.h"
 
 namespace nmspmm {
@@ -50,12 +51,36 @@ __global__ __launch_bounds__(256) void nm_mx4_quantize_kernel(const S *Bc, int64
 
 // ---- the packed weight -----------------------------------------------------
 //
-// Two compressed rows' codes a byte, row-major; the scales; the offsets (none
-// where N = M: row r of a window is its r-th).
+// Where V is a multiple of 16 (and the pattern dense or such that a workgroup's
+// LDS holds the columns of two groups of one row) the codes lie as the lanes of
+// the matrix instruction read them, 16 columns by 32 compressed rows a word
+// (nmspmm_mx4_tile.h), the scales beside them, and the offsets, in the same order,
+// as byte offsets from the group's first window; padding rows have code 0.
+//   dense    four groups (a step) of a column tile in 1 KB, 64 bytes of scales
+//   sparse   one group of CT column tiles in CT * 256 bytes; 32 offsets a block
+// Other widths keep two compressed rows' codes a byte, row-major, the scales and
+// the offsets (none where N = M: row r of a window is its r-th).
+enum class Mx4Kind { Raw, Dense, Sparse };
+
 struct Mx4Layout {
-    int64_t w, q, groups;
+    Mx4Kind kind;
+    int CT;                         // of Sparse
+    int64_t w, q, groups, steps;    // steps: of Dense fours of groups, of Sparse groups
     int64_t scales_at, offs_at, bytes;
 };
+
+// Columns of A that `groups` neighbouring groups can meet, from a multiple of 8 on.
+int64_t mx4_columns(int64_t groups, int64_t k, int N, int M)
+{
+    const int64_t rows = groups * 32, windows = 32 % N == 0 ? rows / N : (rows - 1) / N + 2;
+    return std::min(k, windows * M) + 7;
+}
+
+// Bytes of such a row in LDS: rows start four banks apart.
+int64_t mx4_pitch(int64_t columns) { return round_up(columns * 2, 128) + 16; }
+
+// LDS of the kernel for up to 16 rows: two workgroups a CU, or one.
+constexpr int MX4_LDS = 80 * 1024, MX4_LDS_WIDE = 156 * 1024;
 
 Mx4Layout mx4_layout(int64_t k, int64_t n, int N, int M, int V)
 {
@@ -63,10 +88,69 @@ Mx4Layout mx4_layout(int64_t k, int64_t n, int N, int M, int V)
     l.w = k / M * N;
     l.q = n / V;
     l.groups = (l.w + 31) / 32;
-    l.scales_at = round_up((l.w + 1) / 2 * n, 256);
-    l.offs_at = round_up(l.scales_at + l.groups * n, 256);
-    l.bytes = l.offs_at + (N == M ? 0 : l.w * l.q);
+    const int64_t tiles = n / 16;
+    // (the kernels count compressed rows in 32 bits, and a launch takes fewer than 2^32 threads)
+    const bool fits = V % 16 == 0 && l.w < ((int64_t)1 << 31) - 4096 && n < (int64_t)1 << 27;
+    if (fits && N == M) {
+        l.kind = Mx4Kind::Dense;
+        l.steps = (l.groups + 3) / 4;
+        l.scales_at = tiles * l.steps * 1024;
+        l.offs_at = round_up(l.scales_at + tiles * l.steps * 64, 256);
+        l.bytes = l.offs_at;
+    } else if (fits && mx4_pitch(mx4_columns(2, k, N, M)) <= MX4_LDS / 2) {
+        l.kind = Mx4Kind::Sparse;
+        l.CT = V % 64 == 0 ? 4 : V % 32 == 0 ? 2 : 1;
+        l.steps = l.groups;
+        l.scales_at = tiles * l.steps * 256;
+        l.offs_at = round_up(l.scales_at + tiles / l.CT * l.steps * 16 * l.CT, 256);
+        l.bytes = l.offs_at + l.q * l.steps * 64;
+    } else {
+        l.kind = Mx4Kind::Raw;
+        l.scales_at = round_up((l.w + 1) / 2 * n, 256);
+        l.offs_at = round_up(l.scales_at + l.groups * n, 256);
+        l.bytes = l.offs_at + (N == M ? 0 : l.w * l.q);
+    }
     return l;
+}
+
+// A word of eight codes, a column's scale or an offset of a group a thread and
+// step; once a weight.
+__global__ __launch_bounds__(256) void nm_mx4_pack_kernel(const uint8_t *codes, const uint8_t *scales,
+                                                          const uint8_t *idx, uint8_t *out, Mx4Layout l, int64_t n,
+                                                          int N, int M, int V)
+{
+    const int64_t stride = (int64_t)gridDim.x * 256, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool dense = l.kind == Mx4Kind::Dense;
+    const int per = dense ? 4 : l.CT;           // words of a lane's piece: groups, or column tiles
+    const int64_t pieces = n / 16 * l.steps / (dense ? 1 : per);
+    for (int64_t e = t; e < pieces * 64 * per; e += stride) {
+        const int i = (int)(e % per), lane = (int)(e / per % 64);
+        const int64_t run = e / per / 64 / l.steps, step = e / per / 64 % l.steps;
+        const int64_t group = dense ? step * 4 + i : step;
+        const int64_t j = (dense ? run : run * per + i) * 16 + lane % 16, u0 = group * 32 + lane / 16 * 8;
+        uint32_t word = 0;
+        for (int r = 0; r < 8; ++r)
+            if (u0 + r < l.w) word |= (codes[(u0 + r) * n + j] & 15u) << (4 * r);
+        reinterpret_cast<uint32_t *>(out)[e] = word;
+    }
+    for (int64_t e = t; e < pieces * 16 * per; e += stride) {
+        const int i = (int)(e % per), col = (int)(e / per % 16);
+        const int64_t run = e / per / 16 / l.steps, step = e / per / 16 % l.steps;
+        const int64_t group = dense ? step * 4 + i : step, j = (dense ? run : run * per + i) * 16 + col;
+        out[l.scales_at + e] = group < l.groups ? scales[group * n + j] : (uint8_t)127;
+    }
+    if (dense) return;
+    uint16_t *offs = reinterpret_cast<uint16_t *>(out + l.offs_at);
+    for (int64_t e = t; e < l.q * l.steps * 32; e += stride) {
+        const int64_t block = e / 32 / l.steps, group = e / 32 % l.steps, u = group * 32 + e % 32;
+        uint32_t at = 0;
+        if (u < l.w) {
+            const int o = idx[u * l.q + block];
+            at = (uint32_t)((u / N - group * 32 / N) * M) + (o < M ? o : M - 1);
+        }
+        // rows r and r + 4 of each eight side by side: the lanes' order of both gathers
+        offs[e - e % 8 + e % 4 * 2 + e % 8 / 4] = (uint16_t)(at * 2);
+    }
 }
 
 __global__ __launch_bounds__(256) void nm_mx4_pack_raw_kernel(const uint8_t *codes, const uint8_t *scales,
@@ -138,6 +222,191 @@ hipError_t launch_general(const Mx4GeneralArgs &p, hipStream_t stream)
     return hipGetLastError();
 }
 
+// ---- the kernels for few rows ------------------------------------------------
+
+// The slices of C added in order, then the epilogue, eight columns a thread (n is
+// a multiple of 16 here).
+template <class O>
+__global__ __launch_bounds__(256) void nm_mx4_join_kernel(const float *part, int64_t m, int64_t n, int splits,
+                                                          HalfEpilogue epi)
+{
+    const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (e >= m * n) return;
+    float sum[8] = {}, x[8];
+    for (int s = 0; s < splits; ++s) {
+        load_row<8, true>(part + s * m * n + e, 8, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += x[i];
+    }
+    const int64_t row = e / n;
+    half_store8<O>(epi, row, e - row * n, sum);
+}
+
+struct Mx4Plan {
+    bool general = true;
+    int MT = 1, CT = 1, WC = 1, splits = 1;
+    int rows = 16, chunk = 0, pitch = 0, slot = 0;      // of a workgroup; of a chunk of A
+    bool wide = false;                      // one workgroup a CU
+    int64_t per_split = 0, ws_bytes = 0;
+};
+
+Mx4Plan mx4_plan(int64_t m, const Mx4Layout &l, const nmspmm_mx4_weight_t &w, bool may_split)
+{
+    Mx4Plan c;
+    if (l.kind == Mx4Kind::Raw || l.w == 0) return c;
+    c.general = false;
+    c.MT = m <= 16 ? 1 : m <= 32 ? 2 : 4;
+    const auto pitch = [&](int64_t groups) { return mx4_pitch(mx4_columns(groups, w.k, w.N, w.M)); };
+    if (l.kind == Mx4Kind::Dense) {
+        // one workgroup a CU, as far as four tiles each go (1 x 4096 x 11008, 688 tiles:
+        // CT = 1 to 4 9.4, 8.7, 7.2 and 7.9 us; 1 x 8192 x 8192, 512 tiles: 13.1, 9.0, 9.9, 11.3)
+        c.CT = (int)std::min<int64_t>(4, (w.n / 16 + 255) / 256);
+    } else {
+        c.CT = l.CT;
+        // the k-major kernel, where a slot holds a chunk
+        if (c.MT > 1) {
+            const int64_t most = mx4_wide_columns(c.MT);
+            for (c.WC = 4; c.WC <= 8 && mx4_columns(MX4_NW / c.WC, w.k, w.N, w.M) > most;) c.WC *= 2;
+            if (c.WC > 8) {
+                c.MT = 1;
+            } else {
+                const int WK = MX4_NW / c.WC;
+                int64_t chunk = round_up(l.steps, WK);
+                while (chunk > WK && mx4_columns(chunk, w.k, w.N, w.M) > most) chunk -= WK;
+                c.chunk = (int)chunk;
+            }
+        }
+        if (c.MT == 1) {
+            c.rows = (int)std::min<int64_t>(m, 16);
+            // one workgroup a CU, where A's rows may take all of its LDS, as far as four
+            // runs of tiles each go (13 x 4096 x 11008 at 8:32, 344 runs: WC = 1, 2 and 4
+            // 11.4, 9.1 and 12.7 us; 1 x 8192 x 8192 at 4:32, 128 runs: 5.5, 6.8, 9.4)
+            const int64_t runs = w.n / (16 * l.CT);
+            c.WC = runs <= 256 ? 1 : runs <= 512 ? 2 : 4;
+            c.wide = (runs + c.WC - 1) / c.WC * ((m + c.rows - 1) / c.rows) <= 256;
+            const int64_t lds = c.wide ? MX4_LDS_WIDE : MX4_LDS;
+            for (;; c.WC < 4 ? (void)(c.WC = 4) : (void)(c.rows = (c.rows + 1) / 2)) {
+                const int WK = MX4_NW / c.WC;
+                int64_t chunk = round_up(l.steps, WK);
+                if (c.rows * pitch(chunk) <= lds) {         // all of k
+                    c.slot = (int)lds;
+                } else {
+                    c.slot = (int)lds / 2;
+                    while (chunk > WK && c.rows * pitch(chunk) > c.slot) chunk -= WK;
+                    if (c.rows * pitch(chunk) > c.slot) continue;
+                }
+                c.chunk = (int)chunk;
+                c.pitch = (int)pitch(chunk);
+                break;
+            }
+        }
+    }
+    if (c.MT > 1 || l.kind == Mx4Kind::Dense) c.rows = (int)std::min<int64_t>(m, 16 * c.MT);
+    if (may_split && c.MT > 1) {
+        const int64_t columns = l.kind == Mx4Kind::Dense ? (w.n / 16 + c.CT - 1) / c.CT
+                                                         : (w.n / (16 * c.CT) + c.WC - 1) / c.WC;
+        const int64_t tiles = columns * ((m + 16 * c.MT - 1) / (16 * c.MT));
+        c.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / tiles, l.steps / 8, 16}));
+    }
+    c.per_split = (l.steps + c.splits - 1) / c.splits;
+    c.splits = (int)((l.steps + c.per_split - 1) / c.per_split);
+    c.ws_bytes = c.splits > 1 ? c.splits * m * w.n * 4 : 0;
+    return c;
+}
+
+template <class T, int MT, int CT>
+void launch_dense(const Mx4Args &p, const dim3 &grid, hipStream_t stream)
+{
+    constexpr int D = MT <= 2 ? 2 : 1;
+    if (p.vec) hipLaunchKernelGGL((nm_mx4_dense_kernel<T, MT, CT, D, true>), grid, dim3(MX4_NT), 0, stream, p);
+    else hipLaunchKernelGGL((nm_mx4_dense_kernel<T, MT, CT, 1, false>), grid, dim3(MX4_NT), 0, stream, p);
+}
+
+template <class T, int CT, int WC>
+void launch_short(const Mx4Args &p, const dim3 &grid, bool wide, hipStream_t stream)
+{
+    if (wide) hipLaunchKernelGGL((nm_mx4_sparse_kernel<T, CT, WC, 4, MX4_LDS_WIDE>), grid, dim3(MX4_NT), 0, stream, p);
+    else hipLaunchKernelGGL((nm_mx4_sparse_kernel<T, CT, WC, 4, MX4_LDS>), grid, dim3(MX4_NT), 0, stream, p);
+}
+
+template <class T, int MT, int CT>
+void launch_sparse(const Mx4Plan &c, const Mx4Args &p, const dim3 &grid, hipStream_t stream)
+{
+    if constexpr (MT == 1) {
+        if (c.WC == 1) launch_short<T, CT, 1>(p, grid, c.wide, stream);
+        else if (c.WC == 2) launch_short<T, CT, 2>(p, grid, c.wide, stream);
+        else launch_short<T, CT, 4>(p, grid, c.wide, stream);
+    } else if (c.WC == 4) {
+        hipLaunchKernelGGL((nm_mx4_wide_kernel<T, MT, CT, 4, 4>), grid, dim3(MX4_NT), 0, stream, p);
+    } else {
+        hipLaunchKernelGGL((nm_mx4_wide_kernel<T, MT, CT, 8, 4>), grid, dim3(MX4_NT), 0, stream, p);
+    }
+}
+
+template <class T, int MT>
+void launch_tiles(const Mx4Plan &c, Mx4Kind kind, Mx4Args p, hipStream_t stream)
+{
+    const int run = kind == Mx4Kind::Dense ? c.CT : c.WC;
+    // (a grid takes fewer than 2^16 workgroups along y)
+    const int64_t most = (int64_t)65535 * c.rows;
+    for (; p.first_row < p.m; p.first_row += most) {
+        const dim3 grid((unsigned)((p.tiles + run - 1) / run),
+                        (unsigned)((std::min(most, p.m - p.first_row) + c.rows - 1) / c.rows), (unsigned)c.splits);
+        if (kind == Mx4Kind::Dense) {
+            if (c.CT == 1) launch_dense<T, MT, 1>(p, grid, stream);
+            else if (c.CT == 2) launch_dense<T, MT, 2>(p, grid, stream);
+            else if (c.CT == 3) launch_dense<T, MT, 3>(p, grid, stream);
+            else launch_dense<T, MT, 4>(p, grid, stream);
+        } else {
+            if (c.CT == 1) launch_sparse<T, MT, 1>(c, p, grid, stream);
+            else if (c.CT == 2) launch_sparse<T, MT, 2>(c, p, grid, stream);
+            else launch_sparse<T, MT, 4>(c, p, grid, stream);
+        }
+    }
+}
+
+template <class T>
+hipError_t run_tiles(const Mx4Plan &c, const Mx4Layout &l, const void *A, int64_t lda, const nmspmm_mx4_weight_t &w,
+                     int64_t m, const HalfEpilogue &epi, void *workspace, hipStream_t stream)
+{
+    const unsigned char *base = static_cast<const unsigned char *>(w.packed);
+    Mx4Args p{};
+    p.A = A;
+    p.vals = base;
+    p.scales = base + l.scales_at;
+    p.offs = reinterpret_cast<const uint16_t *>(base + l.offs_at);
+    p.part = static_cast<float *>(workspace);
+    p.lda = lda;
+    p.m = m;
+    p.n = w.n;
+    p.k = w.k;
+    p.w = (int)l.w;
+    p.N = w.N;
+    p.M = w.M;
+    p.V = w.V;
+    p.steps = (int)l.steps;
+    p.per_split = (int)c.per_split;
+    p.tiles = (int)(l.kind == Mx4Kind::Dense ? w.n / 16 : w.n / (16 * l.CT));
+    p.rows = c.rows;
+    p.chunk = c.chunk;
+    p.pitch = c.pitch;
+    p.slot = c.slot;
+    // (the sparse kernel counts a workgroup's bytes of A in 32 bits)
+    p.vec = aligned_to(A, 16) && (m == 1 || lda % 8 == 0) && w.k % 8 == 0 && lda < (int64_t)1 << 23;
+    p.epi = epi;
+    if (c.MT == 1) launch_tiles<T, 1>(c, l.kind, p, stream);
+    else if (c.MT == 2) launch_tiles<T, 2>(c, l.kind, p, stream);
+    else launch_tiles<T, 4>(c, l.kind, p, stream);
+    if (c.splits > 1) {
+        const dim3 grid((unsigned)((m * w.n + 2047) / 2048));
+        if (epi.f32)
+            hipLaunchKernelGGL((nm_mx4_join_kernel<float>), grid, dim3(256), 0, stream, p.part, m, w.n, c.splits, epi);
+        else
+            hipLaunchKernelGGL((nm_mx4_join_kernel<T>), grid, dim3(256), 0, stream, p.part, m, w.n, c.splits, epi);
+    }
+    return hipGetLastError();
+}
+
 nmspmm_status_t check_weight(const nmspmm_mx4_weight_t *w, int64_t m)
 {
     if (!w || !shape_ok(m, w->n, w->k, w->N, w->M, w->V)) return NMSPMM_ERR_INVALID_ARG;
@@ -191,22 +460,35 @@ extern "C" nmspmm_status_t nmspmm_mx4_pack(const uint8_t *codes, const uint8_t *
     if (!aligned_to(w.packed, 256)) return NMSPMM_ERR_UNSUPPORTED;
     const Mx4Layout l = mx4_layout(w.k, w.n, w.N, w.M, w.V);
     const dim3 grid((unsigned)std::min<int64_t>(8192, (l.w * w.n + 511) / 512));
-    hipLaunchKernelGGL(nm_mx4_pack_raw_kernel, grid, dim3(256), 0, stream, codes, scales, idx,
-                       static_cast<uint8_t *>(const_cast<void *>(w.packed)), l, w.n, w.M);
+    uint8_t *out = static_cast<uint8_t *>(const_cast<void *>(w.packed));
+    if (l.kind == Mx4Kind::Raw)
+        hipLaunchKernelGGL(nm_mx4_pack_raw_kernel, grid, dim3(256), 0, stream, codes, scales, idx, out, l, w.n, w.M);
+    else
+        hipLaunchKernelGGL(nm_mx4_pack_kernel, grid, dim3(256), 0, stream, codes, scales, idx, out, l, w.n, w.N, w.M, w.V);
     return hipGetLastError() == hipSuccess ? NMSPMM_OK : NMSPMM_ERR_HIP;
 }
 
 extern "C" int64_t nmspmm_mx4_workspace_bytes(int64_t m, const nmspmm_mx4_weight_t *weight)
 {
-    return check_weight(weight, m) == NMSPMM_OK ? 0 : -1;
+    if (check_weight(weight, m) != NMSPMM_OK) return -1;
+    if (m == 0 || weight->n == 0 || weight->k == 0) return 0;
+    return mx4_plan(m, mx4_layout(weight->k, weight->n, weight->N, weight->M, weight->V), *weight, true).ws_bytes;
 }
 
 extern "C" const char *nmspmm_mx4_kernel_name(int64_t m, const nmspmm_mx4_weight_t *weight, int with_workspace)
 {
     if (check_weight(weight, m) != NMSPMM_OK) return "invalid";
     if (m == 0 || weight->n == 0) return "none";
-    (void)with_workspace;
-    return "nm_mx4_general_kernel";
+    const Mx4Layout l = mx4_layout(weight->k, weight->n, weight->N, weight->M, weight->V);
+    const Mx4Plan c = mx4_plan(m, l, *weight, with_workspace != 0);
+    if (c.general) return "nm_mx4_general_kernel";
+    thread_local char buf[128];
+    if (l.kind == Mx4Kind::Dense)
+        std::snprintf(buf, sizeof buf, "nm_mx4_dense_kernel<mt%d,ct%d>,split%d", c.MT, c.CT, c.splits);
+    else
+        std::snprintf(buf, sizeof buf, "%s<mt%d,ct%d,wc%d>,rows%d,chunk%d,split%d",
+                      c.MT > 1 ? "nm_mx4_wide_kernel" : "nm_mx4_sparse_kernel", c.MT, c.CT, c.WC, c.rows, c.chunk, c.splits);
+    return buf;
 }
 
 extern "C" nmspmm_status_t nmspmm_mx4_run(const void *A, int64_t lda, nmspmm_dtype_t a_dtype,
@@ -231,11 +513,26 @@ extern "C" nmspmm_status_t nmspmm_mx4_run(const void *A, int64_t lda, nmspmm_dty
         !aligned_to(mul, cs) || !aligned_to(residual, cs) || !aligned_to(workspace, 256))
         return NMSPMM_ERR_UNSUPPORTED;
     if (!sizes_fit(m, std::max({ldc, ld_mul, ld_residual}), lda)) return NMSPMM_ERR_UNSUPPORTED;
-    (void)workspace_bytes;
     const Mx4Layout l = mx4_layout(w.k, w.n, w.N, w.M, w.V);
-    const HalfEpilogue epi = {C, bias, mul, residual, ldc, ld_mul, ld_residual, alpha, act, c_dtype == NMSPMM_F32, false};
-    const Mx4GeneralArgs p{A, static_cast<const unsigned char *>(w.packed), l, m == 1 ? w.k : lda, m, w.n, w.N, w.M,
-                           w.V, epi};
-    const hipError_t e = a_dtype == NMSPMM_BF16 ? launch_general<bf16_t>(p, stream) : launch_general<f16_t>(p, stream);
-    return e == hipSuccess ? NMSPMM_OK : NMSPMM_ERR_HIP;
+    if (m == 1) lda = w.k;
+    const auto rows16 = [cs](const void *ptr, int64_t ld) { return !ptr || (aligned_to(ptr, 16) && ld * cs % 16 == 0); };
+    const HalfEpilogue epi = {C, bias, mul, residual, ldc, ld_mul, ld_residual, alpha, act, c_dtype == NMSPMM_F32,
+                              rows16(C, ldc) && rows16(mul, ld_mul) && rows16(residual, ld_residual) &&
+                                  aligned_to(bias, 16)};
+    int cached = -1;
+    Mx4Plan c = mx4_plan(m, l, w, true);
+    if (c.ws_bytes > 0 && (!workspace || (uint64_t)c.ws_bytes > (uint64_t)workspace_bytes)) {
+        workspace = capturing(stream) ? nullptr : ws_acquire(stream, (size_t)c.ws_bytes, &cached);
+        if (!workspace) c = mx4_plan(m, l, w, false);
+    }
+    hipError_t e;
+    if (c.general) {
+        const Mx4GeneralArgs p{A, static_cast<const unsigned char *>(w.packed), l, lda, m, w.n, w.N, w.M, w.V, epi};
+        e = a_dtype == NMSPMM_BF16 ? launch_general<bf16_t>(p, stream) : launch_general<f16_t>(p, stream);
+    } else {
+        e = a_dtype == NMSPMM_BF16 ? run_tiles<bf16_t>(c, l, A, lda, w, m, epi, workspace, stream)
+                                   : run_tiles<f16_t>(c, l, A, lda, w, m, epi, workspace, stream);
+    }
+    const hipError_t f = cached >= 0 ? ws_done(cached, stream) : hipSuccess;
+    return e == hipSuccess && f == hipSuccess ? NMSPMM_OK : NMSPMM_ERR_HIP;
 }
