@@ -246,6 +246,12 @@ void launch_attend4(const AttendArgs &p, const Kv4Pages &f, int GT, unsigned gro
     else launch_attend4_heads<64>(p, f, GT, groups, stream);
 }
 
+// Whether the matrix-core kernel takes the cache.
+bool attend4_takes_mfma(const nmspmm_kv4_cache_t *c)
+{
+    return c->page_size % 4 == 0 && c->dim <= 256 && kv4_layout(c->page_size, c->dim).block < (int64_t)1 << 31;
+}
+
 nmspmm_status_t check_attend4_sizes(const nmspmm_kv4_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window)
 {
     const nmspmm_status_t st = check_kv4(c);
@@ -318,7 +324,7 @@ extern "C" int64_t nmspmm_kv4_attend_workspace_bytes(const nmspmm_kv4_cache_t *c
     if (check_attend4_sizes(cache, q_heads, max_length, window) != NMSPMM_OK) return -1;
     if (q_heads == 0 || cache->sequences == 0) return 0;
     const nmspmm_kv_cache_t sizes = kv4_sizes(cache);
-    return attend_plan(&sizes, q_heads, max_length, window, false, true).bytes;
+    return attend_plan(&sizes, q_heads, max_length, window, attend4_takes_mfma(cache), true).bytes;
 }
 
 extern "C" nmspmm_status_t nmspmm_kv4_attend(const nmspmm_kv4_cache_t *cache, const void *q, const int64_t *q_stride,
@@ -340,10 +346,11 @@ extern "C" nmspmm_status_t nmspmm_kv4_attend(const nmspmm_kv4_cache_t *cache, co
         return NMSPMM_ERR_UNSUPPORTED;
     const nmspmm_kv_cache_t sizes = kv4_sizes(cache);
     int cached = -1;
-    AttendPlan a = attend_plan(&sizes, q_heads, max_length, window, false, true);
+    const bool mfma = attend4_takes_mfma(cache);
+    AttendPlan a = attend_plan(&sizes, q_heads, max_length, window, mfma, true);
     if (a.bytes > 0 && (!workspace || (uint64_t)a.bytes > (uint64_t)workspace_bytes)) {
         workspace = capturing(stream) ? nullptr : ws_acquire(stream, (size_t)a.bytes, &cached);
-        if (!workspace) a = attend_plan(&sizes, q_heads, max_length, window, false, false);
+        if (!workspace) a = attend_plan(&sizes, q_heads, max_length, window, mfma, false);
     }
     AttendArgs p{};
     p.c = device_view(&sizes);
@@ -369,7 +376,8 @@ extern "C" nmspmm_status_t nmspmm_kv4_attend(const nmspmm_kv4_cache_t *cache, co
     p.io = dtype;
     p.q_vec = rows_aligned(q, q_stride, 2, cache->dim, es);
     const Kv4Pages f = kv4_view(cache);
-    launch_attend4(p, f, a.GT, (unsigned)a.groups, stream);
+    if (mfma) launch_attend4_mfma(p, f, cache->page_size % 16 == 0, (unsigned)a.groups, stream);
+    else launch_attend4(p, f, a.GT, (unsigned)a.groups, stream);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
         launch_join(p, a.rows, stream);
