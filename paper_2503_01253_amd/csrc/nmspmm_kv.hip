@@ -271,7 +271,7 @@ __global__ __launch_bounds__(AT_NT) void nm_attend_kernel(AttendArgs p)
     }
 }
 
-constexpr int JN_SPLITS = 2048, JN_U = 4;
+constexpr int JN_U = 4;
 
 // The parts of a split sequence joined, one query head a workgroup: the
 // weights of all splits first, then DL threads take a split's dimensions and
@@ -372,13 +372,10 @@ void launch_join(const AttendArgs &p, int64_t rows, hipStream_t stream)
 AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window, bool mfma,
                        bool split)
 {
-    AttendPlan a{};
     const int64_t group = q_heads / c->heads;
-    a.GT = mfma ? ATTEND_MFMA_HEADS : group >= 5 ? 8 : group >= 3 ? 4 : (int)group;
-    a.gtiles = (int)((group + a.GT - 1) / a.GT);
-    int64_t span = std::min({max_length, table_positions(c), KV_MAX_LENGTH});
-    if (window > 0) span = std::min(span, window);
-    const int64_t base = c->sequences * c->heads * a.gtiles;
+    const int GT = mfma ? ATTEND_MFMA_HEADS : group >= 5 ? 8 : group >= 3 ? 4 : (int)group;
+    const int64_t span = attend_span(c, max_length, window);
+    const int64_t base = c->sequences * c->heads * ((group + GT - 1) / GT);
     // eight workgroups a CU (two or three run at once), each of 256 positions at
     // least; and of 1024 at most, for batches whose lengths differ, which only
     // the device knows (192 sequences of 0 to 5000 positions, 64 heads on 8: 273
@@ -389,15 +386,7 @@ AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_
         splits = std::max<int64_t>(1, std::min<int64_t>((JN_SPLITS + base - 1) / base, span / 256));
         splits = std::max(splits, std::min<int64_t>({JN_SPLITS, (span + 1023) / 1024, 16384 / base}));
     }
-    a.chunk = (int)std::max<int64_t>(128, ((span + splits - 1) / splits + 127) / 128 * 128);
-    a.splits = (int)std::max<int64_t>(1, (span + a.chunk - 1) / a.chunk);     // 1 where splits is
-    a.groups = base * a.splits;
-    a.rows = c->sequences * q_heads;
-    if (a.splits > 1) {
-        a.ml_bytes = (a.rows * a.splits * 8 + 255) / 256 * 256;
-        a.bytes = a.ml_bytes + a.rows * a.splits * c->dim * 4;
-    }
-    return a;
+    return attend_cut(c, q_heads, span, GT, splits);
 }
 
 namespace {

@@ -75,9 +75,9 @@ nmspmm_status_t check_kv4(const nmspmm_kv4_cache_t *c);
 nmspmm_status_t check_kv4_pointers(const nmspmm_kv4_cache_t *c);
 Kv4Pages kv4_view(const nmspmm_kv4_cache_t *c);
 
-// nmspmm_kv4_mfma.hip: pages of whole fours of tokens (uniform: of sixteens), a head's
-// block under 2^31 bytes, at most 256 dimensions; tiles of ATTEND_MFMA_HEADS heads.
-void launch_attend4_mfma(const AttendArgs &p, const Kv4Pages &f, bool uniform, unsigned groups, hipStream_t stream);
+// nmspmm_kv4_mfma.hip: pages of whole fours of tokens, a head's block under 2^31
+// bytes, at most 256 dimensions; tiles of ATTEND_MFMA_HEADS heads.
+void launch_attend4_mfma(const AttendArgs &p, const Kv4Pages &f, int page_size, unsigned groups, hipStream_t stream);
 
 }  // namespace nmspmm
 

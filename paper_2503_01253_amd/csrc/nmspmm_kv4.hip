@@ -252,6 +252,32 @@ bool attend4_takes_mfma(const nmspmm_kv4_cache_t *c)
     return c->page_size % 4 == 0 && c->dim <= 256 && kv4_layout(c->page_size, c->dim).block < (int64_t)1 << 31;
 }
 
+// How the work is cut.  For the matrix-core kernel, of which a CU holds four
+// workgroups: into what runs at once, where that leaves chunks of 256 to 2048
+// positions (one sequence of 131071 on 8 heads 37.5 us, in twice as many chunks 43);
+// else into quarters of the longest, 1024 to 2048 positions each, for batches whose
+// lengths differ (48 sequences of 0 to 5000, in chunks of 1792, 1280 and 640: 42.3,
+// 37.5 and 40 us; 128 of 8192, in chunks of 2048, 1408 and 1024: 218, 225 and 233).
+AttendPlan attend4_plan(const nmspmm_kv4_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window, bool split)
+{
+    const nmspmm_kv_cache_t sizes = kv4_sizes(c);
+    if (!attend4_takes_mfma(c)) return attend_plan(&sizes, q_heads, max_length, window, false, split);
+    const int64_t span = attend_span(&sizes, max_length, window);
+    const int64_t base = c->sequences * c->heads * ((q_heads / c->heads + ATTEND_MFMA_HEADS - 1) / ATTEND_MFMA_HEADS);
+    int64_t splits = 1;
+    if (split && base > 0) {
+        splits = 1024 / base;
+        if (splits == 0 || span > 2048 * splits) {
+            const int64_t most = std::max<int64_t>(1024, std::min<int64_t>(2048, (span / 4 + 127) / 128 * 128));
+            // (up to 64 workgroups a CU, which bounds the workspace)
+            splits = std::max<int64_t>(1, std::min<int64_t>({JN_SPLITS, (span + most - 1) / most, 16384 / base}));
+        } else {
+            splits = std::max<int64_t>(1, std::min(splits, span / 256));
+        }
+    }
+    return attend_cut(&sizes, q_heads, span, ATTEND_MFMA_HEADS, splits);
+}
+
 nmspmm_status_t check_attend4_sizes(const nmspmm_kv4_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window)
 {
     const nmspmm_status_t st = check_kv4(c);
@@ -323,8 +349,7 @@ extern "C" int64_t nmspmm_kv4_attend_workspace_bytes(const nmspmm_kv4_cache_t *c
 {
     if (check_attend4_sizes(cache, q_heads, max_length, window) != NMSPMM_OK) return -1;
     if (q_heads == 0 || cache->sequences == 0) return 0;
-    const nmspmm_kv_cache_t sizes = kv4_sizes(cache);
-    return attend_plan(&sizes, q_heads, max_length, window, attend4_takes_mfma(cache), true).bytes;
+    return attend4_plan(cache, q_heads, max_length, window, true).bytes;
 }
 
 extern "C" nmspmm_status_t nmspmm_kv4_attend(const nmspmm_kv4_cache_t *cache, const void *q, const int64_t *q_stride,
@@ -347,10 +372,10 @@ extern "C" nmspmm_status_t nmspmm_kv4_attend(const nmspmm_kv4_cache_t *cache, co
     const nmspmm_kv_cache_t sizes = kv4_sizes(cache);
     int cached = -1;
     const bool mfma = attend4_takes_mfma(cache);
-    AttendPlan a = attend_plan(&sizes, q_heads, max_length, window, mfma, true);
+    AttendPlan a = attend4_plan(cache, q_heads, max_length, window, true);
     if (a.bytes > 0 && (!workspace || (uint64_t)a.bytes > (uint64_t)workspace_bytes)) {
         workspace = capturing(stream) ? nullptr : ws_acquire(stream, (size_t)a.bytes, &cached);
-        if (!workspace) a = attend_plan(&sizes, q_heads, max_length, window, mfma, false);
+        if (!workspace) a = attend4_plan(cache, q_heads, max_length, window, false);
     }
     AttendArgs p{};
     p.c = device_view(&sizes);
@@ -376,7 +401,7 @@ extern "C" nmspmm_status_t nmspmm_kv4_attend(const nmspmm_kv4_cache_t *cache, co
     p.io = dtype;
     p.q_vec = rows_aligned(q, q_stride, 2, cache->dim, es);
     const Kv4Pages f = kv4_view(cache);
-    if (mfma) launch_attend4_mfma(p, f, cache->page_size % 16 == 0, (unsigned)a.groups, stream);
+    if (mfma) launch_attend4_mfma(p, f, cache->page_size, (unsigned)a.groups, stream);
     else launch_attend4(p, f, a.GT, (unsigned)a.groups, stream);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {

@@ -17,6 +17,11 @@
 //                 two tokens together: nothing goes through LDS.
 // The next tokens' codes are on their way meanwhile, their pages looked up before.
 // The waves are joined in LDS.
+// 128 x 8192 positions, 32 heads on 8 of 128, 218-228 us (5.0-5.2 TB/s), one sequence of
+// 131071, 64 heads on 8, 38-41 with its joining (3.6 TB/s).  A tile of 32 tokens takes a
+// SIMD some 230 vector and 32 matrix instructions, 0.5 us of them alone, and 4.3 KB, 0.2
+// us at the HBM's rate: four waves a SIMD keep enough of them on their way.  Two tiles
+// ahead a wave took the registers of a fourth wave (219 -> 225 us).
 #include "nmspmm_kv4.h"
 
 namespace nmspmm {
@@ -83,9 +88,9 @@ __device__ __forceinline__ float group_scale(const uint32_t *bytes)
 }
 
 // DK: groups of a row, 1 to 4, or 8 for any number from 5 to 8.  QP: parts of a
-// query value.  UNI: pages of whole sixteens of tokens, so that a tile's page is the
-// same for all lanes.
-template <int DK, int QP, bool UNI>
+// query value.  PIECE: pages are of whole pieces of 16, 8 or 4 tokens.  The pages of
+// pieces of 16 and 8 are looked up once a wave, those of 4 by every lane for itself.
+template <int DK, int QP, int PIECE>
 __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2 : 3) void nm_attend4_mfma_kernel(AttendArgs p, Kv4Pages f)
 {
     constexpr int GT = ATTEND_MFMA_HEADS, PP = 3;
@@ -95,7 +100,91 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
     constexpr int NT = VU * NI, AP = DK * 32 + 4, SW = DK > 4 ? 2 : 1;
     __shared__ __align__(16) float acc[A4M_NW * GT * AP];
     __shared__ float2 s_ml[A4M_NW][GT];
-    const AttendTask t = attend_task(p, blockIdx.x, GT);
+    // A sequence's chunks start at one that differs from sequence to sequence: in the
+    // same order, where their number divides the CUs', a CU meets first chunks only, or
+    // last ones, which few sequences fill (192 sequences of 0 to 5000 positions in four
+    // chunks 130 us, so 97).
+    const uint32_t tiles = p.gtiles * p.heads, run = blockIdx.x / tiles, seq = run / p.splits;
+    const uint32_t split = (run % p.splits + (seq * 0x9e3779b1u >> 20)) % p.splits;
+    const AttendTask t = attend_task(p, (seq * p.splits + split) * tiles + blockIdx.x % tiles, GT);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int col = lane & 15, grp = lane >> 4;
+    const int G = DK == 8 ? f.l.G : DK;
+
+    // ---- the tokens.  What lies outside the chunk or in no page is left out by its
+    // score and by zeros for its values: loads go to a place that is there (the
+    // table's last position, the cache's first page) and wait for no comparison ----
+    const int32_t *row = p.c.table + t.seq * p.c.table_stride;
+    const unsigned char *blocks = f.pages + t.head * f.l.block;
+    const int end = p.c.pages > 0 ? t.end : 0, last = p.cap - 1;
+    // of the tile's pieces of PIECE tokens (4: of this lane's keys, then of its values):
+    // the table's entries and the slots
+    constexpr int PIECES = PIECE == 4 ? 4 : 32 / PIECE;
+    struct Where {
+        int32_t page[PIECES], slot[PIECES];
+    };
+    auto look_up = [&](int base) {
+        Where w;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int pos = base + (PIECE > 4 ? i * PIECE : i < 2 ? 16 * i + col : 16 * (i - 2) + 4 * grp);
+            const uint32_t in = (uint32_t)min(pos, last), at = p.c.size.div(in);
+            w.page[i] = row[at];
+            w.slot[i] = (int32_t)(in - at * p.c.size.d);
+            if (PIECE > 4) w.slot[i] &= ~(PIECE - 1);       // (past the end: the last piece)
+        }
+        return w;
+    };
+    // (selections, no branches: what is selected is there)
+    const uint32_t pages = (uint32_t)p.c.pages;
+    auto held = [&](int32_t page) { return (uint32_t)page < pages; };
+    // Where piece i starts, `at` bytes into its page's block and `unit` bytes a slot on:
+    // the same for all lanes (but with pieces of 4), to which a lane adds its own bytes.
+    auto start = [&](const Where &w, int i, int64_t at, uint32_t slots, uint32_t unit) {
+        return blocks + (int64_t)(held(w.page[i]) ? w.page[i] : 0) * f.stride + at + slots * unit;
+    };
+    // of sixteen s, what a lane reads for its token (keys) or its four tokens (values)
+    auto place = [&](const Where &w, int s, bool values, int64_t at, uint32_t unit, uint32_t mine) {
+        const int shift = values ? 2 : 0;       // values: slots by fours
+        if constexpr (PIECE == 16) return start(w, s, at, (uint32_t)w.slot[s] >> shift, unit) + mine;
+        else if constexpr (PIECE == 8) {
+            const unsigned char *one = start(w, 2 * s, at, (uint32_t)w.slot[2 * s] >> shift, unit);
+            const unsigned char *two = start(w, 2 * s + 1, at, (uint32_t)w.slot[2 * s + 1] >> shift, unit);
+            return ((values ? grp > 1 : col > 7) ? two : one) + mine;
+        } else {
+            const int i = (values ? 2 : 0) + s;
+            return start(w, i, at, (uint32_t)w.slot[i] >> shift, unit) + mine;
+        }
+    };
+    const uint32_t k_slot = PIECE == 16 ? col : PIECE == 8 ? col & 7 : 0, v_quad = PIECE == 16 ? grp : PIECE == 8 ? grp & 1 : 0;
+    const uint32_t k_mine = k_slot * (16 * G) + grp * G * 4, ks_mine = k_slot * f.l.sp;
+    uint32_t v_mine[VU], vs_mine[VU];
+#pragma unroll
+    for (int u = 0; u < VU; ++u) {
+        // (lanes past a row's words read the last: their sums are not stored)
+        const int D = min(col % LD + 16 * u, 4 * G - 1);
+        v_mine[u] = v_quad * (64 * G) + D * 16;
+        vs_mine[u] = v_quad * (4 * G) + D / 4 * 4;
+    }
+    // a bit for every token of the tile at base: in the chunk, and (with pieces of 4:
+    // where this lane holds its values) in a page
+    auto tokens = [&](const Where &w, int base) {
+        const int lo = t.begin - base, hi = end - base;
+        uint32_t bits = hi >= 32 ? ~0u : hi > 0 ? (1u << hi) - 1 : 0u;
+        if (lo > 0) bits &= lo < 32 ? ~0u << lo : 0u;
+        uint32_t there = 0;
+#pragma unroll
+        for (int i = 0; i < (PIECE == 4 ? 2 : PIECES); ++i) {
+            const uint32_t of = PIECE == 16 ? 0xffffu : PIECE == 8 ? 0xffu : 0xfu << (4 * grp);
+            const int page = w.page[PIECE == 4 ? 2 + i : i];
+            there |= held(page) ? of << (PIECE == 4 ? 16 * i : PIECE * i) : 0u;
+        }
+        if (PIECE == 4) there |= ~(0xf000fu << (4 * grp));      // (other lanes' tokens)
+        return bits & there;
+    };
+    // the first tile's entries are asked for together with the sequence's length
+    Where first;
+    if (p.cap > 0 && p.window == 0) first = look_up(t.split * p.chunk + wave * A4M_TOKENS);
     if (t.begin >= t.end && p.splits > 1) {      // nothing here: the maximum says so
         if (threadIdx.x < t.heads_in_tile) {
             const int64_t row = t.seq * ((int64_t)p.heads * p.group) + t.first_head + threadIdx.x;
@@ -103,92 +192,22 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
         }
         return;
     }
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int col = lane & 15, grp = lane >> 4;
-    const int G = DK == 8 ? f.l.G : DK;
 
-    s16x8 q[QP][DK];
-#pragma unroll
-    for (int c = 0; c < DK; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int d = c * 32 + grp * 8 + j;
-            const bool there = col < t.heads_in_tile && d < p.dim;
-            const int64_t at = t.seq * p.qs[0] + (t.first_head + col) * p.qs[1] + d;
-            if constexpr (QP == 1) {
-                if (p.q_vec) {      // eight at once
-                    if (j == 0) {
-                        q[0][c] = s16x8{0, 0, 0, 0, 0, 0, 0, 0};
-                        if (there) q[0][c] = *reinterpret_cast<const s16x8 *>(static_cast<const short *>(p.q) + at);
-                    }
-                    continue;
-                }
-                q[0][c][j] = there ? static_cast<const short *>(p.q)[at] : (short)0;
-            } else {
-                const float x = !there ? 0.f : p.io == NMSPMM_F32 ? static_cast<const float *>(p.q)[at]
-                                                                  : to_f32(static_cast<const f16_t *>(p.q)[at]);
-                short part[QP];
-                split_parts<QP>(x, part);
-#pragma unroll
-                for (int i = 0; i < QP; ++i) q[i][c][j] = part[i];
-            }
-        }
-
-    // ---- the tokens ----
-    const int32_t *row = p.c.table + t.seq * p.c.table_stride;
-    const unsigned char *blocks = f.pages + t.head * f.l.block;
-    struct Where {      // of the tile's two sixteens: pages (-1: none) and slots of this lane's keys and values
-        int32_t k_page[2], v_page[2], k_slot[2], v_slot[2];
-    };
-    auto find = [&](int pos, int32_t &page, int32_t &slot) {
-        page = -1, slot = 0;
-        if (pos < t.end) {
-            const Place at = place_of(p.c, row, pos);
-            page = at.held ? (int32_t)at.page : -1;
-            slot = at.slot;
-        }
-    };
-    auto look_up = [&](int base) {
-        Where w;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            if constexpr (UNI) {
-                find(base + 16 * s, w.k_page[s], w.k_slot[s]);
-                w.k_page[s] = __builtin_amdgcn_readfirstlane(w.k_page[s]);
-                w.k_slot[s] = __builtin_amdgcn_readfirstlane(w.k_slot[s]);
-                w.v_page[s] = w.k_page[s];
-                w.v_slot[s] = w.k_slot[s];
-            } else {
-                find(base + 16 * s + col, w.k_page[s], w.k_slot[s]);
-                find(base + 16 * s + 4 * grp, w.v_page[s], w.v_slot[s]);
-            }
-        }
-        return w;
-    };
-    uint32_t kw[2][DK], ks[2][SW];
+    uint32_t kw[2][DK], ks[2][SW], vs[2][VU];
     u32x4 vw[2][VU];
-    uint32_t vs[2][VU];
     auto load_k = [&](const Where &w) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-#pragma unroll
-            for (int c = 0; c < DK; ++c) kw[s][c] = 0;
-#pragma unroll
-            for (int i = 0; i < SW; ++i) ks[s][i] = 0x7f7f7f7fu;
-            if (w.k_page[s] < 0) continue;
-            const unsigned char *b = blocks + w.k_page[s] * f.stride;
-            const uint32_t slot = (uint32_t)w.k_slot[s] + (UNI ? col : 0);
-            const unsigned char *at = b + slot * (uint32_t)(16 * G) + (uint32_t)(grp * G * 4);
+            const unsigned char *at = place(w, s, false, 0, 16 * G, k_mine);
             if constexpr (DK <= 4) {
                 __builtin_memcpy(kw[s], __builtin_assume_aligned(at, 4 * (DK & -DK)), 4 * DK);
             } else {
                 if (G == 8) __builtin_memcpy(kw[s], __builtin_assume_aligned(at, 16), 32);
                 else
 #pragma unroll
-                    for (int c = 0; c < DK; ++c)
-                        if (c < G) kw[s][c] = *reinterpret_cast<const uint32_t *>(at + 4 * c);
+                    for (int c = 0; c < DK; ++c) kw[s][c] = c < G ? *reinterpret_cast<const uint32_t *>(at + 4 * c) : 0u;
             }
-            const unsigned char *sc = b + f.l.ks_at + slot * (uint32_t)f.l.sp;
+            const unsigned char *sc = place(w, s, false, f.l.ks_at, f.l.sp, ks_mine);
             if constexpr (DK == 1) ks[s][0] = *sc;
             else if constexpr (DK == 2) ks[s][0] = *reinterpret_cast<const uint16_t *>(sc);
             else __builtin_memcpy(ks[s], __builtin_assume_aligned(sc, 4 * SW), 4 * SW);
@@ -199,15 +218,36 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int u = 0; u < VU; ++u) {
-                const int D = col % LD + 16 * u;
-                vw[s][u] = u32x4{0, 0, 0, 0};
-                vs[s][u] = 0x7f7f7f7fu;
-                if (w.v_page[s] < 0 || ((DK == 3 || DK == 8) && D >= 4 * G)) continue;
-                const unsigned char *b = blocks + w.v_page[s] * f.stride;
-                const uint32_t quad = (uint32_t)w.v_slot[s] / 4 + (UNI ? grp : 0);
-                vw[s][u] = *reinterpret_cast<const u32x4 *>(b + f.l.v_at + quad * (uint32_t)(64 * G) + (uint32_t)(D * 16));
-                vs[s][u] = *reinterpret_cast<const uint32_t *>(b + f.l.vs_at + quad * (uint32_t)(4 * G) + (uint32_t)(D / 4 * 4));
+                vw[s][u] = *reinterpret_cast<const u32x4 *>(place(w, s, true, f.l.v_at, 64 * G, v_mine[u]));
+                vs[s][u] = *reinterpret_cast<const uint32_t *>(place(w, s, true, f.l.vs_at, 4 * G, vs_mine[u]));
             }
+    };
+
+    s16x8 q[QP][DK];
+    auto load_q = [&]() {
+#pragma unroll
+        for (int c = 0; c < DK; ++c) {
+            const int d = c * 32 + grp * 8, valid = col < t.heads_in_tile ? p.dim - d : 0;
+            const int64_t at = t.seq * p.qs[0] + (t.first_head + col) * p.qs[1] + d;
+            float x[8];
+            if constexpr (QP == 1) {
+                if (p.q_vec) load_row<8, true>(static_cast<const bf16_t *>(p.q) + at, valid, x);
+                else load_row<8, false>(static_cast<const bf16_t *>(p.q) + at, valid, x);
+            } else if constexpr (QP == 2) {
+                if (p.q_vec) load_row<8, true>(static_cast<const f16_t *>(p.q) + at, valid, x);
+                else load_row<8, false>(static_cast<const f16_t *>(p.q) + at, valid, x);
+            } else {
+                if (p.q_vec && p.dim % 8 == 0) load_row<8, true>(static_cast<const float *>(p.q) + at, valid, x);
+                else load_row<8, false>(static_cast<const float *>(p.q) + at, valid, x);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                short part[QP];
+                split_parts<QP>(x[j], part);
+#pragma unroll
+                for (int i = 0; i < QP; ++i) q[i][c][j] = part[i];
+            }
+        }
     };
 
     f32x4 o[NT];
@@ -217,10 +257,15 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
 
     int base = (t.begin & ~(A4M_TOKENS - 1)) + wave * A4M_TOKENS;
     constexpr int STEP = A4M_NW * A4M_TOKENS;
-    Where cur = look_up(base), next = look_up(base + STEP);
-    load_k(cur);
-    load_v(cur);
-    for (; base < t.end; base += STEP) {
+    Where cur, next;        // of the tile that is in the registers, and of the one after it
+    if (base < end) {
+        cur = p.window > 0 ? look_up(base) : first;
+        next = look_up(base + STEP);
+        load_k(cur);
+        load_v(cur);
+    }
+    load_q();
+    for (; base < end; base += STEP) {
         f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
         auto group = [&](auto index) {
             constexpr int c = decltype(index)::value;
@@ -247,17 +292,17 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = s[j / 4][j % 4] * p.scale2;
         // tokens outside the chunk, or of no page: no weight, and zeros for values
-        const bool whole = base >= t.begin && base + A4M_TOKENS <= t.end && cur.v_page[0] >= 0 && cur.v_page[1] >= 0;
-        if (!(UNI ? whole : __all(whole))) {
+        const uint32_t bits = tokens(cur, base);
+        if (PIECE == 4 ? __any(bits != ~0u) : bits != ~0u) {
+            const int mine = (int)(bits >> (grp * 4));
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int pos = base + j / 4 * 16 + grp * 4 + j % 4;
-                if (pos >= t.begin && pos < t.end && cur.v_page[j / 4] >= 0) continue;
-                x[j] = NEG_INF;
+                const uint32_t in = (uint32_t)(mine << (31 - (j / 4 * 16 + j % 4)) >> 31);     // all ones, or none
+                x[j] = in ? x[j] : NEG_INF;
 #pragma unroll
                 for (int u = 0; u < VU; ++u) {
-                    vw[j / 4][u][j % 4] = 0;
-                    vs[j / 4][u] = (vs[j / 4][u] & ~(0xffu << (j % 4 * 8))) | 0x7fu << (j % 4 * 8);
+                    vw[j / 4][u][j % 4] &= in;
+                    vs[j / 4][u] &= in | ~(0x80u << (j % 4 * 8));      // a scale that is not NaN
                 }
             }
         }
@@ -360,31 +405,32 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
 }
 
 template <int DK, int QP>
-void launch(const AttendArgs &p, const Kv4Pages &f, bool uniform, unsigned groups, hipStream_t stream)
+void launch(const AttendArgs &p, const Kv4Pages &f, int page_size, unsigned groups, hipStream_t stream)
 {
     const dim3 grid(groups), block(A4M_NT);
-    if (uniform) hipLaunchKernelGGL((nm_attend4_mfma_kernel<DK, QP, true>), grid, block, 0, stream, p, f);
-    else hipLaunchKernelGGL((nm_attend4_mfma_kernel<DK, QP, false>), grid, block, 0, stream, p, f);
+    if (page_size % 16 == 0) hipLaunchKernelGGL((nm_attend4_mfma_kernel<DK, QP, 16>), grid, block, 0, stream, p, f);
+    else if (page_size % 8 == 0) hipLaunchKernelGGL((nm_attend4_mfma_kernel<DK, QP, 8>), grid, block, 0, stream, p, f);
+    else hipLaunchKernelGGL((nm_attend4_mfma_kernel<DK, QP, 4>), grid, block, 0, stream, p, f);
 }
 
 template <int QP>
-void launch_groups(const AttendArgs &p, const Kv4Pages &f, bool uniform, unsigned groups, hipStream_t stream)
+void launch_groups(const AttendArgs &p, const Kv4Pages &f, int page_size, unsigned groups, hipStream_t stream)
 {
-    if (f.l.G == 1) launch<1, QP>(p, f, uniform, groups, stream);
-    else if (f.l.G == 2) launch<2, QP>(p, f, uniform, groups, stream);
-    else if (f.l.G == 3) launch<3, QP>(p, f, uniform, groups, stream);
-    else if (f.l.G == 4) launch<4, QP>(p, f, uniform, groups, stream);
-    else launch<8, QP>(p, f, uniform, groups, stream);
+    if (f.l.G == 1) launch<1, QP>(p, f, page_size, groups, stream);
+    else if (f.l.G == 2) launch<2, QP>(p, f, page_size, groups, stream);
+    else if (f.l.G == 3) launch<3, QP>(p, f, page_size, groups, stream);
+    else if (f.l.G == 4) launch<4, QP>(p, f, page_size, groups, stream);
+    else launch<8, QP>(p, f, page_size, groups, stream);
 }
 
 }  // namespace
 
 // A bf16 query is one part, an fp16 one two (16 bits), an fp32 one three (24).
-void launch_attend4_mfma(const AttendArgs &p, const Kv4Pages &f, bool uniform, unsigned groups, hipStream_t stream)
+void launch_attend4_mfma(const AttendArgs &p, const Kv4Pages &f, int page_size, unsigned groups, hipStream_t stream)
 {
-    if (p.io == NMSPMM_BF16) launch_groups<1>(p, f, uniform, groups, stream);
-    else if (p.io == NMSPMM_F16) launch_groups<2>(p, f, uniform, groups, stream);
-    else launch_groups<3>(p, f, uniform, groups, stream);
+    if (p.io == NMSPMM_BF16) launch_groups<1>(p, f, page_size, groups, stream);
+    else if (p.io == NMSPMM_F16) launch_groups<2>(p, f, page_size, groups, stream);
+    else launch_groups<3>(p, f, page_size, groups, stream);
 }
 
 }  // namespace nmspmm

@@ -75,7 +75,33 @@ struct AttendPlan {
 // nmspmm_kv.hip.  mfma: tiles of 16 query heads; split: sequences may be cut.
 AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window, bool mfma,
                        bool split);
+
+// The positions of a sequence that a call may attend to, at most.
+inline int64_t attend_span(const nmspmm_kv_cache_t *c, int64_t max_length, int64_t window)
+{
+    const int64_t span = std::min({max_length, table_positions(c), KV_MAX_LENGTH});
+    return window > 0 ? std::min(span, window) : span;
+}
+
+// The plan with tiles of GT heads and about `splits` chunks of whole 128 positions.
+inline AttendPlan attend_cut(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t span, int GT, int64_t splits)
+{
+    AttendPlan a{};
+    a.GT = GT;
+    a.gtiles = (int)((q_heads / c->heads + GT - 1) / GT);
+    a.chunk = (int)std::max<int64_t>(128, ((span + splits - 1) / splits + 127) / 128 * 128);
+    a.splits = (int)std::max<int64_t>(1, (span + a.chunk - 1) / a.chunk);     // 1 where splits is
+    a.groups = c->sequences * c->heads * a.gtiles * a.splits;
+    a.rows = c->sequences * q_heads;
+    if (a.splits > 1) {
+        a.ml_bytes = (a.rows * a.splits * 8 + 255) / 256 * 256;
+        a.bytes = a.ml_bytes + a.rows * a.splits * c->dim * 4;
+    }
+    return a;
+}
+
 nmspmm_status_t check_attend_sizes(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window);
+constexpr int JN_SPLITS = 2048;     // most chunks of a sequence
 void launch_join(const AttendArgs &p, int64_t rows, hipStream_t stream);     // the parts of split sequences joined
 
 }  // namespace nmspmm

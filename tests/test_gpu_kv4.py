@@ -320,6 +320,36 @@ def test_attend_leaves_out_pages_outside_the_cache(dim, page):
     assert torch.all((out - want).abs() <= 2.0 ** -18 * (want.abs() + 1))      # order of the sums
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128, 256])
+@pytest.mark.parametrize("page", [8, 24, 16, 4, 5, 32])
+def test_attend_counts_the_positions_that_are_there(page, dim, dtype):
+    """With a scale of 0 every position weighs 1: the log-sum-exp counts them,
+    over tables whose pages are there, one or all missing, at lengths that end
+    inside and at the end of a page."""
+    say(f"[kv4 attend] counts {page} {dim} {dtype}")
+    rng = np.random.default_rng(6)
+    heads, group, pages = 2, 4, 5
+    pool = pool_of(pages, page, heads, dim)
+    whole = nm.nmspmm_kv4_cache(pool, torch.arange(pages, dtype=torch.int32, device="cuda")[None], page, heads, dim)
+    k, v = (tensor(rng, (pages * page, heads, dim), "f32") for _ in range(2))
+    pos = torch.arange(pages * page, dtype=torch.int32, device="cuda")
+    nm.nmspmm_kv4_append(whole, k, v, torch.zeros_like(pos), pos)
+    tables = [[-5, 7, 9, 5, -1], [4, -1, 2 ** 31 - 1, -2 ** 31, 5], [-1, 4, -1, -1, -1], [-1, -1, 4, -1, -1],
+              [-1, -1, -1, -1, 4], [0, 1, 2, 3, 4], [3, 2, -1, 1, 0]]
+    handle = nm.nmspmm_kv4_cache(pool, torch.tensor(tables, dtype=torch.int32).cuda(), page, heads, dim)
+    q = tensor(rng, (len(tables), heads * group, dim), dtype)
+    out, lse = torch.empty_like(q), torch.empty(len(tables), heads * group, device="cuda")
+    for length in (1, page, page + 1, 2 * page, 3 * page - 1, 5 * page):
+        for window in (0, 1, page, 2 * page + 1):
+            nm.nmspmm_kv4_attend(handle, q, torch.full((len(tables),), length, dtype=torch.int32, device="cuda"), out,
+                                 lse=lse, scale=0.0, window=window)
+            first = max(0, length - window) if window else 0
+            want = [sum(0 <= table[i // page] < pages for i in range(first, length)) for table in tables]
+            got = np.exp(f64(lse))
+            assert np.all(np.abs(got - np.array(want)[:, None]) <= 1e-4 * np.array(want)[:, None]), (length, window)
+
+
 def test_attend_a_row_of_infinite_scores():
     """Keys whose scores are all minus infinity (q of -3e38 times k of 2^125): a zero
     row with lse minus infinity; a NaN group inside the range makes its heads NaN,
