@@ -73,7 +73,7 @@ struct Mx4Layout {
 int64_t mx4_columns(int64_t groups, int64_t k, int N, int M)
 {
     const int64_t rows = groups * 32, windows = 32 % N == 0 ? rows / N : (rows - 1) / N + 2;
-    return std::min(k, windows * M) + 7;
+    return std::min(k, windows * M) + (M % 8 ? 7 : 0);
 }
 
 // Bytes of such a row in LDS: rows start four banks apart.
@@ -224,27 +224,40 @@ hipError_t launch_general(const Mx4GeneralArgs &p, hipStream_t stream)
 
 // ---- the kernels for few rows ------------------------------------------------
 
-// The slices of C added in order, then the epilogue, eight columns a thread (n is
-// a multiple of 16 here).
-template <class O>
-__global__ __launch_bounds__(256) void nm_mx4_join_kernel(const float *part, int64_t m, int64_t n, int splits,
+// The slices of C added in order, then the epilogue, four columns a thread (n is
+// a multiple of 16 here): eight slices' loads, and those of the epilogue, on their
+// way at once (64 x 4096 from 8 slices and a term 4.7 us; one slice after another 12).
+template <class T>
+__global__ __launch_bounds__(128) void nm_mx4_join_kernel(const float *part, int64_t m, int64_t n, int splits,
                                                           HalfEpilogue epi)
 {
-    const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    const int64_t e = ((int64_t)blockIdx.x * 128 + threadIdx.x) * 4;
     if (e >= m * n) return;
-    float sum[8] = {}, x[8];
-    for (int s = 0; s < splits; ++s) {
-        load_row<8, true>(part + s * m * n + e, 8, x);
+    const int64_t row = e / n, j = e - row * n;
+    const Mx4Ahead ahead = mx4_fetch<T>(epi, row, j);
+    float sum[4] = {};
+    for (int s0 = 0; s0 < splits; s0 += 8) {
+        float x[8][4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += x[i];
+        for (int s = 0; s < 8; ++s) load_row<4, true>(part + min(s0 + s, splits - 1) * m * n + e, 4, x[s]);
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += s0 + s < splits ? x[s][i] : 0.f;
     }
-    const int64_t row = e / n;
-    half_store8<O>(epi, row, e - row * n, sum);
+    mx4_emit<T>(epi, row, j, sum, ahead);
 }
+
+}  // namespace
+
+// nmspmm_mx4_wide.hip
+void launch_mx4_wide(int MT, int CT, int WC, int D, bool bf16, const Mx4Args &p, const dim3 &grid, hipStream_t stream);
+
+namespace {
 
 struct Mx4Plan {
     bool general = true;
-    int MT = 1, CT = 1, WC = 1, splits = 1;
+    int MT = 1, CT = 1, WC = 1, D = 0, splits = 1;
     int rows = 16, chunk = 0, pitch = 0, slot = 0;      // of a workgroup; of a chunk of A
     bool wide = false;                      // one workgroup a CU
     int64_t per_split = 0, ws_bytes = 0;
@@ -258,23 +271,21 @@ Mx4Plan mx4_plan(int64_t m, const Mx4Layout &l, const nmspmm_mx4_weight_t &w, bo
     c.MT = m <= 16 ? 1 : m <= 32 ? 2 : 4;
     const auto pitch = [&](int64_t groups) { return mx4_pitch(mx4_columns(groups, w.k, w.N, w.M)); };
     if (l.kind == Mx4Kind::Dense) {
-        // one workgroup a CU, as far as four tiles each go (1 x 4096 x 11008, 688 tiles:
+        // one workgroup a CU, as far as four tiles each go; more than 16 rows, of which
+        // every workgroup reads all of A: four (1 x 4096 x 11008, 688 tiles:
         // CT = 1 to 4 9.4, 8.7, 7.2 and 7.9 us; 1 x 8192 x 8192, 512 tiles: 13.1, 9.0, 9.9, 11.3)
-        c.CT = (int)std::min<int64_t>(4, (w.n / 16 + 255) / 256);
+        c.CT = c.MT > 1 ? 4 : (int)std::min<int64_t>(4, (w.n / 16 + 255) / 256);
     } else {
         c.CT = l.CT;
-        // the k-major kernel, where a slot holds a chunk
+        // the k-major kernel, where a slot holds a chunk: D groups of each of the waves that
+        // share columns
         if (c.MT > 1) {
-            const int64_t most = mx4_wide_columns(c.MT);
-            for (c.WC = 4; c.WC <= 8 && mx4_columns(MX4_NW / c.WC, w.k, w.N, w.M) > most;) c.WC *= 2;
-            if (c.WC > 8) {
-                c.MT = 1;
-            } else {
-                const int WK = MX4_NW / c.WC;
-                int64_t chunk = round_up(l.steps, WK);
-                while (chunk > WK && mx4_columns(chunk, w.k, w.N, w.M) > most) chunk -= WK;
-                c.chunk = (int)chunk;
-            }
+            for (c.WC = 4; c.WC <= 8 && c.D == 0; c.WC *= 2)
+                for (int D = c.WC == 4 ? 4 : 1; D >= 1 && c.D == 0; D /= 2)
+                    if (mx4_columns(D * (MX4_NW / c.WC), w.k, w.N, w.M) <= mx4_wide_columns(c.MT)) c.D = D;
+            c.WC /= 2;
+            c.chunk = c.D * (MX4_NW / c.WC);
+            if (c.D == 0) c.MT = 1;
         }
         if (c.MT == 1) {
             c.rows = (int)std::min<int64_t>(m, 16);
@@ -306,6 +317,9 @@ Mx4Plan mx4_plan(int64_t m, const Mx4Layout &l, const nmspmm_mx4_weight_t &w, bo
         const int64_t columns = l.kind == Mx4Kind::Dense ? (w.n / 16 + c.CT - 1) / c.CT
                                                          : (w.n / (16 * c.CT) + c.WC - 1) / c.WC;
         const int64_t tiles = columns * ((m + 16 * c.MT - 1) / (16 * c.MT));
+        // k in slices where the tiles leave CUs idle, of eight steps at least (64 x 11008 x
+        // 4096 at 16:32, 32 tiles: 1, 2, 4 and 8 slices 54, 36, 25 and 18 us; 40 x 4096 x
+        // 11008 at 4:32, 86 tiles, 16 steps: 1, 2 and 4 15.4, 14 and 21)
         c.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / tiles, l.steps / 8, 16}));
     }
     c.per_split = (l.steps + c.splits - 1) / c.splits;
@@ -336,10 +350,8 @@ void launch_sparse(const Mx4Plan &c, const Mx4Args &p, const dim3 &grid, hipStre
         if (c.WC == 1) launch_short<T, CT, 1>(p, grid, c.wide, stream);
         else if (c.WC == 2) launch_short<T, CT, 2>(p, grid, c.wide, stream);
         else launch_short<T, CT, 4>(p, grid, c.wide, stream);
-    } else if (c.WC == 4) {
-        hipLaunchKernelGGL((nm_mx4_wide_kernel<T, MT, CT, 4, 4>), grid, dim3(MX4_NT), 0, stream, p);
     } else {
-        hipLaunchKernelGGL((nm_mx4_wide_kernel<T, MT, CT, 8, 4>), grid, dim3(MX4_NT), 0, stream, p);
+        launch_mx4_wide(MT, CT, c.WC, c.D, __is_same(T, bf16_t), p, grid, stream);
     }
 }
 
@@ -350,8 +362,8 @@ void launch_tiles(const Mx4Plan &c, Mx4Kind kind, Mx4Args p, hipStream_t stream)
     // (a grid takes fewer than 2^16 workgroups along y)
     const int64_t most = (int64_t)65535 * c.rows;
     for (; p.first_row < p.m; p.first_row += most) {
-        const dim3 grid((unsigned)((p.tiles + run - 1) / run),
-                        (unsigned)((std::min(most, p.m - p.first_row) + c.rows - 1) / c.rows), (unsigned)c.splits);
+        const dim3 grid((unsigned)((p.tiles + run - 1) / run * c.splits),
+                        (unsigned)((std::min(most, p.m - p.first_row) + c.rows - 1) / c.rows));
         if (kind == Mx4Kind::Dense) {
             if (c.CT == 1) launch_dense<T, MT, 1>(p, grid, stream);
             else if (c.CT == 2) launch_dense<T, MT, 2>(p, grid, stream);
@@ -385,6 +397,7 @@ hipError_t run_tiles(const Mx4Plan &c, const Mx4Layout &l, const void *A, int64_
     p.M = w.M;
     p.V = w.V;
     p.steps = (int)l.steps;
+    p.splits = c.splits;
     p.per_split = (int)c.per_split;
     p.tiles = (int)(l.kind == Mx4Kind::Dense ? w.n / 16 : w.n / (16 * l.CT));
     p.rows = c.rows;
@@ -398,11 +411,8 @@ hipError_t run_tiles(const Mx4Plan &c, const Mx4Layout &l, const void *A, int64_
     else if (c.MT == 2) launch_tiles<T, 2>(c, l.kind, p, stream);
     else launch_tiles<T, 4>(c, l.kind, p, stream);
     if (c.splits > 1) {
-        const dim3 grid((unsigned)((m * w.n + 2047) / 2048));
-        if (epi.f32)
-            hipLaunchKernelGGL((nm_mx4_join_kernel<float>), grid, dim3(256), 0, stream, p.part, m, w.n, c.splits, epi);
-        else
-            hipLaunchKernelGGL((nm_mx4_join_kernel<T>), grid, dim3(256), 0, stream, p.part, m, w.n, c.splits, epi);
+        const dim3 grid((unsigned)((m * w.n + 511) / 512));
+        hipLaunchKernelGGL((nm_mx4_join_kernel<T>), grid, dim3(128), 0, stream, p.part, m, w.n, c.splits, epi);
     }
     return hipGetLastError();
 }

@@ -29,7 +29,9 @@ struct Mx4Args {
     float *part;                // with split k: splits x m x n partial sums
     int64_t lda, m, n, k, first_row;
     int32_t w, N, M, V;
-    int32_t steps, per_split;   // groups (dense: steps of four) of all of k, and of a slice
+    int32_t steps;              // groups (dense: steps of four) of all of k
+    int32_t splits, per_split;  // slices of k (neighbouring workgroups: a slice's are on one XCD, which
+                                // reads its part of A once), and the steps of one
     int32_t tiles;              // runs of CT column tiles (dense: column tiles)
     int32_t rows;               // rows of a workgroup, 16 MT at most
     int32_t chunk;              // sparse: groups of a chunk of A (a multiple of WK)
@@ -80,19 +82,71 @@ __device__ __forceinline__ void mx4_group(const s16x8 (&a)[MT], uint32_t w, floa
     }
 }
 
-// What the epilogue reads for a thread's first output, asked for at the kernel's
-// start (for one row: all of it; the last reads of a kernel that is bound by latency).
+// What the epilogue reads for four columns of a row.
 struct Mx4Ahead {
+    float bias[4], mul[4], residual[4];
+};
+
+template <class O, bool VEC>
+__device__ __forceinline__ void mx4_fetch_of(const HalfEpilogue &e, int64_t r, int64_t j, Mx4Ahead &a)
+{
+    if (e.bias) load_row<4, VEC>(e.bias + j, 4, a.bias);
+    if (e.mul) load_row<4, VEC>(static_cast<const O *>(e.mul) + r * e.ld_mul + j, 4, a.mul);
+    if (e.residual) load_row<4, VEC>(static_cast<const O *>(e.residual) + r * e.ld_residual + j, 4, a.residual);
+}
+
+template <class T>
+__device__ __forceinline__ Mx4Ahead mx4_fetch(const HalfEpilogue &e, int64_t r, int64_t j)
+{
+    Mx4Ahead a{};
+    if (e.f32) e.vec ? mx4_fetch_of<float, true>(e, r, j, a) : mx4_fetch_of<float, false>(e, r, j, a);
+    else e.vec ? mx4_fetch_of<T, true>(e, r, j, a) : mx4_fetch_of<T, false>(e, r, j, a);
+    return a;
+}
+
+// The epilogue of four sums.
+template <class T>
+__device__ __forceinline__ void mx4_emit(const HalfEpilogue &e, int64_t r, int64_t j, const float (&sum)[4],
+                                         const Mx4Ahead &a)
+{
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = e.alpha * sum[i] + (e.bias ? a.bias[i] : 0.f);
+    if (e.act != NMSPMM_HALF_ACT_NONE) {
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {       // (one copy of the activations' code)
+            float v = half_act(y[0], e.act);
+            y[0] = y[1], y[1] = y[2], y[2] = y[3], y[3] = v;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (e.mul) y[i] *= a.mul[i];
+        if (e.residual) y[i] += a.residual[i];
+    }
+    if (e.f32) {
+        float *dst = static_cast<float *>(e.C) + r * e.ldc + j;
+        e.vec ? store_row<4, true>(dst, 4, y) : store_row<4, false>(dst, 4, y);
+    } else {
+        T *dst = static_cast<T *>(e.C) + r * e.ldc + j;
+        e.vec ? store_row<4, true>(dst, 4, y) : store_row<4, false>(dst, 4, y);
+    }
+}
+
+// Up to 16 rows: what the epilogue reads for a thread's first output, asked for at the
+// kernel's start (for one row: all of it; the last reads of a kernel that latency bounds:
+// 1 x 4096 x 4096, dense, 5.4 -> 4.8 us).
+struct Mx4First {
     float bias, mul, residual;
 };
 
 template <class T, int COLS>
-__device__ __forceinline__ Mx4Ahead mx4_ahead(const Mx4Args &p, int64_t row0, int64_t col0, int rows, bool split)
+__device__ __forceinline__ Mx4First mx4_first(const Mx4Args &p, int64_t row0, int64_t col0, int rows, bool split)
 {
-    Mx4Ahead a{0.f, 1.f, 0.f};
+    Mx4First a{0.f, 1.f, 0.f};
     const int row = threadIdx.x / COLS;
     const int64_t r = row0 + row, j = col0 + threadIdx.x % COLS;
-    if (split || row >= min(rows, 16) || j >= p.n) return a;
+    if (split || row >= rows || j >= p.n) return a;
     if (p.epi.bias) a.bias = p.epi.bias[j];
     if (p.epi.mul) {
         const int64_t at = r * p.epi.ld_mul + j;
@@ -108,7 +162,7 @@ __device__ __forceinline__ Mx4Ahead mx4_ahead(const Mx4Args &p, int64_t row0, in
 
 // half_store with those.
 template <class O>
-__device__ __forceinline__ void mx4_store(const HalfEpilogue &e, int64_t i, int64_t j, float sum, const Mx4Ahead &a)
+__device__ __forceinline__ void mx4_store(const HalfEpilogue &e, int64_t i, int64_t j, float sum, const Mx4First &a)
 {
     float y = e.alpha * sum;
     if (e.bias) y += a.bias;
@@ -119,37 +173,68 @@ __device__ __forceinline__ void mx4_store(const HalfEpilogue &e, int64_t i, int6
 }
 
 // The sums of the WK waves that share columns, added in their order, and the
-// epilogue (or, with k in slices, the slice's partial sums).  A tile row of 16
-// rows at a time; wave wk * WC + wc holds columns wc * CT * 16 and on.
+// epilogue (or, with k in slices, the slice's partial sums).  Wave wk * WC + wc holds
+// columns wc * CT * 16 and on; red holds MX4_NW * CT * MT * 256 floats.  Up to 16 rows
+// one output a thread, more than 16 four columns, MX4_U times at once (64 x 4096 at k =
+// 512 one after another 15 us, so 8.4; 1 x 4096 x 11008, dense, 7.2 and so 9.2).
+constexpr int MX4_U = 4;
+
 template <class T, int MT, int CT, int WC>
 __device__ __forceinline__ void mx4_finish(const Mx4Args &p, float *red, const f32x4 (&acc)[CT][MT], int64_t row0,
-                                           int64_t col0, int valid_rows, bool split, const Mx4Ahead &ahead)
+                                           int64_t col0, int rows, bool split, const Mx4First &ahead)
 {
     constexpr int WK = MX4_NW / WC, COLS = WC * CT * 16;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    lds_sync();
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        lds_sync();
+    for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int c = 0; c < CT; ++c)
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) red[((wave * CT + c) * 4 + e) * 64 + lane] = acc[c][t][e];
-        lds_sync();
-        const int rows = min(16, valid_rows - t * 16);
+            for (int e = 0; e < 4; ++e) red[(((wave * CT + c) * MT + t) * 4 + e) * 64 + lane] = acc[c][t][e];
+    lds_sync();
+    const int64_t part = split ? ((int64_t)(blockIdx.x % p.splits) * p.m + row0) * p.n : 0;
+    if constexpr (MT == 1) {
         for (int i = tid; i < rows * COLS; i += MX4_NT) {
             const int row = i / COLS, col = i % COLS;
             const float *x = red + ((col / 16) * 4 + row % 4) * 64 + row / 4 * 16 + col % 16;
             float sum = 0.f;
 #pragma unroll
             for (int k = 0; k < WK; ++k) sum += x[k * (WC * CT * 256)];
-            const int64_t r = row0 + t * 16 + row, j = col0 + col;
+            const int64_t r = row0 + row, j = col0 + col;
             if (j >= p.n) continue;
-            if (split) p.part[((int64_t)blockIdx.z * p.m + r) * p.n + j] = sum;
-            else if (t == 0 && i == tid) {
+            if (split) p.part[part + row * p.n + j] = sum;
+            else if (i == tid) {
                 if (p.epi.f32) mx4_store<float>(p.epi, r, j, sum, ahead);
                 else mx4_store<T>(p.epi, r, j, sum, ahead);
             } else if (p.epi.f32) half_store<float>(p.epi, r, j, sum);
             else half_store<T>(p.epi, r, j, sum);
+        }
+    } else {
+        for (int first = tid; first < rows * COLS / 4; first += MX4_NT * MX4_U) {
+            Mx4Ahead a[MX4_U];
+#pragma unroll
+            for (int u = 0; u < MX4_U; ++u) {
+                const int i = first + u * MX4_NT, row = i * 4 / COLS;
+                const int64_t j = col0 + i * 4 % COLS;
+                if (!split && row < rows && j < p.n) a[u] = mx4_fetch<T>(p.epi, row0 + row, j);
+            }
+#pragma unroll
+            for (int u = 0; u < MX4_U; ++u) {
+                const int i = first + u * MX4_NT, row = i * 4 / COLS, col = i * 4 % COLS;
+                const int64_t j = col0 + col;
+                if (row >= rows || j >= p.n) continue;
+                const float *x = red + (((col / 16) * MT + row / 16) * 4 + row % 4) * 64 + row % 16 / 4 * 16 + col % 16;
+                float sum[4] = {};
+#pragma unroll
+                for (int k = 0; k < WK; ++k) {
+                    const f32x4 v = *reinterpret_cast<const f32x4 *>(x + k * (WC * CT * MT * 256));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) sum[q] += v[q];
+                }
+                if (split) *reinterpret_cast<f32x4 *>(p.part + part + row * p.n + j) = f32x4{sum[0], sum[1], sum[2], sum[3]};
+                else mx4_emit<T>(p.epi, row0 + row, j, sum, a[u]);
+            }
         }
     }
 }
@@ -162,16 +247,17 @@ __device__ __forceinline__ void mx4_finish(const Mx4Args &p, float *red, const f
 template <class T, int MT, int CT, int D, bool VEC>
 __global__ __launch_bounds__(MX4_NT, MT == 1 && VEC ? 4 : 2) void nm_mx4_dense_kernel(Mx4Args p)
 {
-    __shared__ __align__(16) float red[MX4_NW * CT * 256];
+    __shared__ __align__(16) float red[MX4_NW * CT * MT * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
     const int64_t row0 = p.first_row + (int64_t)blockIdx.y * p.rows;
     const int rows = (int)min64(p.rows, p.m - row0);
-    const int first = blockIdx.z * p.per_split, last = min(first + p.per_split, p.steps) - 1;
+    const int column = p.splits > 1 ? blockIdx.x / p.splits : blockIdx.x, slice = blockIdx.x - column * p.splits;
+    const int first = slice * p.per_split, last = min(first + p.per_split, p.steps) - 1;
     const unsigned char *vals[CT], *scales[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-        const int64_t tile = min((int)blockIdx.x * CT + c, p.tiles - 1);
+        const int64_t tile = min(column * CT + c, p.tiles - 1);
         vals[c] = p.vals + tile * p.steps * 1024 + lane * 16;
         scales[c] = p.scales + tile * p.steps * 64 + col * 4;
     }
@@ -179,9 +265,9 @@ __global__ __launch_bounds__(MX4_NT, MT == 1 && VEC ? 4 : 2) void nm_mx4_dense_k
 #pragma unroll
     for (int t = 0; t < MT; ++t) a_row[t] = static_cast<const T *>(p.A) + (row0 + min(t * 16 + col, rows - 1)) * p.lda;
 
-    const bool split = p.per_split < p.steps;
-    const int64_t col0 = (int64_t)blockIdx.x * (CT * 16);
-    const Mx4Ahead ahead = mx4_ahead<T, CT * 16>(p, row0, col0, rows, split);
+    const bool split = p.splits > 1;
+    const int64_t col0 = (int64_t)column * (CT * 16);
+    const Mx4First ahead = MT == 1 ? mx4_first<T, CT * 16>(p, row0, col0, rows, split) : Mx4First{};
     u32x4 rv[D][CT];
     uint32_t rs[D][CT];
     s16x8 ra[D][4][MT];
@@ -285,16 +371,17 @@ __global__ __launch_bounds__(MX4_NT, LDS <= 80 * 1024 ? 4 : 2) void nm_mx4_spars
     const int col = lane & 15, grp = lane >> 4, wc = wave % WC, wk = wave / WC;
     const int64_t row0 = p.first_row + (int64_t)blockIdx.y * p.rows;
     const int rows = (int)min64(p.rows, p.m - row0);
-    const int first = blockIdx.z * p.per_split, end = min(first + p.per_split, p.steps);
-    const int64_t tile = min((int)blockIdx.x * WC + wc, p.tiles - 1);
+    const int column = p.splits > 1 ? blockIdx.x / p.splits : blockIdx.x, slice = blockIdx.x - column * p.splits;
+    const int first = slice * p.per_split, end = min(first + p.per_split, p.steps);
+    const int64_t tile = min(column * WC + wc, p.tiles - 1);
     const unsigned char *vals = p.vals + tile * p.steps * (256 * CT) + lane * (4 * CT);
     const unsigned char *scales = p.scales + tile * p.steps * (16 * SP) + col * SP;
     const unsigned char *offs = reinterpret_cast<const unsigned char *>(p.offs) +
                                 (tile * (CT * 16) / p.V) * p.steps * 64 + grp * 16;
 
-    const bool split = p.per_split < p.steps;
-    const int64_t col0 = (int64_t)blockIdx.x * (WC * CT * 16);
-    const Mx4Ahead ahead = mx4_ahead<T, WC * CT * 16>(p, row0, col0, rows, split);
+    const bool split = p.splits > 1;
+    const int64_t col0 = (int64_t)column * (WC * CT * 16);
+    const Mx4First ahead = mx4_first<T, WC * CT * 16>(p, row0, col0, rows, split);
     uint32_t rv[D][CT], rs[D];
     u32x4 ro[D];
     auto load = [&](int i, int step) {
@@ -375,35 +462,37 @@ __global__ __launch_bounds__(MX4_NT, LDS <= 80 * 1024 ? 4 : 2) void nm_mx4_spars
     mx4_finish<T, 1, CT, WC>(p, reinterpret_cast<float *>(lds), acc, row0, col0, rows, split, ahead);
 }
 
-// Columns of A that a slot of the kernel below holds.
-constexpr int mx4_wide_columns(int MT) { return MX4_NT * 32 / (16 * MT); }
+// Columns of A that a slot of the kernel below holds, and its threads' blocks of A.
+constexpr int MX4_NB = 2;
+__host__ __device__ constexpr int mx4_wide_columns(int MT) { return MX4_NB * MX4_NT * 32 / (16 * MT); }
 
 // Sparse, 16 MT rows.  As above, but that A_s holds columns: LDS row c has column c
 // of the chunk, its 16 MT rows in granules of 16 (32 bytes) of which the t-th lies
-// at place t ^ swizzle(c).  A slab comes through registers, a block of 4 rows and 8
-// columns a thread, transposed by byte permutes; the next one is on its way meanwhile.
-template <class T, int MT, int CT, int WC, int D>
-__global__ __launch_bounds__(MX4_NT, MT * CT > 8 ? 2 : 4) void nm_mx4_wide_kernel(Mx4Args p)
+// at place t ^ swizzle(c).  A slab comes through registers, NB blocks of 4 rows and 8
+// columns a thread, transposed by byte permutes; the next two are on their way
+// meanwhile.
+template <class T, int MT, int CT, int WC, int D, bool VEC>
+__global__ __launch_bounds__(MX4_NT, 2) void nm_mx4_wide_kernel(Mx4Args p)
 {
-    constexpr int WK = MX4_NW / WC, SP = CT, BM = 16 * MT, PITCH = 2 * BM, SWZ = MT - 1;
-    constexpr int SLOT = mx4_wide_columns(MT) * PITCH;
-    static_assert((MT == 2 || MT == 4) && MX4_NW * CT * 1024 <= 2 * SLOT, "the joining of the waves");
+    constexpr int WK = MX4_NW / WC, SP = CT, CHUNK = D * WK, BM = 16 * MT, PITCH = 2 * BM, SWZ = MT - 1;
+    constexpr int SLOT = mx4_wide_columns(MT) * PITCH, NB = MX4_NB, AD = 2;
+    static_assert((MT == 2 || MT == 4) && MX4_NW * CT * MT * 1024 <= 2 * SLOT, "the joining of the waves");
     __shared__ __align__(256) unsigned char lds[2 * SLOT];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, grp = lane >> 4, wc = wave % WC, wk = wave / WC;
     const int64_t row0 = p.first_row + (int64_t)blockIdx.y * p.rows;
     const int rows = (int)min64(p.rows, p.m - row0);
-    const int first = blockIdx.z * p.per_split, end = min(first + p.per_split, p.steps);
-    const int64_t tile = min((int)blockIdx.x * WC + wc, p.tiles - 1);
+    const int column = p.splits > 1 ? blockIdx.x / p.splits : blockIdx.x, slice = blockIdx.x - column * p.splits;
+    const int first = slice * p.per_split, end = min(first + p.per_split, p.steps);
+    const int64_t tile = min(column * WC + wc, p.tiles - 1);
     const unsigned char *vals = p.vals + tile * p.steps * (256 * CT) + lane * (4 * CT);
     const unsigned char *scales = p.scales + tile * p.steps * (16 * SP) + col * SP;
     // a lane's two rows of the group's: 8 grp + r and 4 further, r = lane / 4 % 4
     const unsigned char *offs = reinterpret_cast<const unsigned char *>(p.offs) +
                                 (tile * (CT * 16) / p.V) * p.steps * 64 + grp * 16 + (lane >> 2 & 3) * 4;
 
-    const bool split = p.per_split < p.steps;
-    const int64_t col0 = (int64_t)blockIdx.x * (WC * CT * 16);
-    const Mx4Ahead ahead = mx4_ahead<T, WC * CT * 16>(p, row0, col0, rows, split);
+    const bool split = p.splits > 1;
+    const int64_t col0 = (int64_t)column * (WC * CT * 16);
     uint32_t rv[D][CT], rs[D], ro[D];
     auto load = [&](int i, int step) {
         const int64_t s = min(step, end - 1);
@@ -417,44 +506,57 @@ __global__ __launch_bounds__(MX4_NT, MT * CT > 8 ? 2 : 4) void nm_mx4_wide_kerne
     // ---- A: this thread's block of a slab, rows 4 rb and on, columns 8 kc and on (16 lanes
     // take four pieces of four blocks of rows, which a write finds on different banks) ----
     const T *A = static_cast<const T *>(p.A) + row0 * p.lda;
-    const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(A, p.vec ? (uint32_t)(((rows - 1) * p.lda + p.k) * 2) : 0u);
-    const int rb = ((tid >> 2) & 3) + 4 * ((tid >> 5) % MT), kc = (tid & 3) + 4 * ((tid >> 4) & 1) + 8 * (tid / (2 * BM));
-    u32x4 ra[4];
-    auto load_a = [&](int s0) {
-        const int64_t c0 = mx4_chunk_base(p, s0) + kc * 8, c1 = mx4_chunk_end(p, min(s0 + p.chunk, end));
-        if (p.vec) {
+    const __amdgpu_buffer_rsrc_t a_rsrc = make_rsrc(A, VEC ? (uint32_t)(((rows - 1) * p.lda + p.k) * 2) : 0u);
+    const int rb = ((tid >> 2) & 3) + 4 * ((tid >> 5) % MT), kc0 = (tid & 3) + 4 * ((tid >> 4) & 1) + 8 * (tid / (2 * BM));
+    constexpr int KB = mx4_wide_columns(MT) / NB / 8;     // pieces of 8 columns from one block of a thread to its next
+    u32x4 ra[AD][NB][4];
+    uint32_t a_off[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                ra[r] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                    a_rsrc, (int)(c0 < c1 && 4 * rb + r < rows ? (uint32_t)(((4 * rb + r) * p.lda + c0) * 2) : OOB), 0, 0));
-        } else {
+    for (int r = 0; r < 4; ++r)
+        a_off[r] = 4 * rb + r < rows ? (uint32_t)((4 * rb + r) * p.lda * 2) + kc0 * 16 : OOB;
+    // (columns past the chunk's are no group's; past the last row's end they read zeros)
+    auto load_a = [&](int d, int s0) {
+        const int64_t base = mx4_chunk_base(p, min(s0, end));
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+        for (int b = 0; b < NB; ++b) {
+            if constexpr (VEC) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t two[2];
+                for (int r = 0; r < 4; ++r)
+                    ra[d][b][r] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                        a_rsrc, (int)a_off[r], (int)(base * 2) + b * KB * 16, 0));
+            } else {
+                const int64_t c0 = base + (kc0 + b * KB) * 8;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int64_t c = c0 + 2 * j + h;
-                        two[h] = c < c1 && 4 * rb + r < rows
-                                     ? __builtin_bit_cast(uint16_t, A[(4 * rb + r) * p.lda + c]) : 0u;
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t two[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int64_t c = c0 + 2 * j + h;
+                            two[h] = c < p.k && 4 * rb + r < rows
+                                         ? __builtin_bit_cast(uint16_t, A[(4 * rb + r) * p.lda + c]) : 0u;
+                        }
+                        ra[d][b][r][j] = two[0] | two[1] << 16;
                     }
-                    ra[r][j] = two[0] | two[1] << 16;
-                }
+            }
         }
     };
     auto swizzle = [](int c) { return (c ^ (c >> 3)) & SWZ; };
-    auto store_a = [&](int slot) {
+    auto store_a = [&](int d, int slot) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            u32x2 out[4];
-            transpose_4x4(ra, half, out);
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c = kc * 8 + 4 * half + j;
-                *reinterpret_cast<u32x2 *>(lds + slot * SLOT + c * PITCH + (((rb >> 2) ^ swizzle(c)) << 5) + 8 * (rb & 3)) = out[j];
+            for (int half = 0; half < 2; ++half) {
+                u32x2 out[4];
+                transpose_4x4(ra[d][b], half, out);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = (kc0 + b * KB) * 8 + 4 * half + j;
+                    *reinterpret_cast<u32x2 *>(lds + slot * SLOT + c * PITCH + (((rb >> 2) ^ swizzle(c)) << 5) +
+                                               8 * (rb & 3)) = out[j];
+                }
             }
-        }
     };
 
     f32x4 acc[CT][MT];
@@ -486,30 +588,30 @@ __global__ __launch_bounds__(MX4_NT, MT * CT > 8 ? 2 : 4) void nm_mx4_wide_kerne
         for (int c = 0; c < CT; ++c) mx4_group<T, MT>(a, rv[i][c], mx4_scale_at(rs[i], c), acc[c]);
     };
 
-    load_a(first);
+    load_a(0, first);
 #pragma unroll
     for (int i = 0; i < D; ++i) load(i, first + wk + i * WK);
-    int slot = 1, chunk_end = first;
-    int64_t c0 = 0;
-    for (int s0 = first; s0 < end; s0 += D * WK) {
+    load_a(1, first + CHUNK);
+    // a chunk: its slab, which has been on its way for AD chunks, into the other slot
+    // (whose readers were through at the last barrier), the next one asked for; then D
+    // groups a wave
+    auto chunk = [&](int d, int s0, int slot) {
+        store_a(d, slot);
+        lds_sync();
+        const int64_t c0 = mx4_chunk_base(p, s0);
 #pragma unroll
         for (int i = 0; i < D; ++i) {
-            const int s = s0 + i * WK;
-            if (s >= end) break;
-            if (s == chunk_end) {
-                // the other slot's readers were through at the last such place
-                slot ^= 1;
-                store_a(slot);
-                lds_sync();
-                c0 = mx4_chunk_base(p, s);
-                chunk_end = s + p.chunk;
-                if (chunk_end < end) load_a(chunk_end);
-            }
-            compute(i, s + wk, c0, slot);
-            load(i, s + wk + D * WK);
+            compute(i, s0 + wk + i * WK, c0, slot);
+            load(i, s0 + CHUNK + wk + i * WK);
         }
+        load_a(d, s0 + AD * CHUNK);     // (last: a wait for the weight's loads is none for these)
+    };
+    for (int s0 = first; s0 < end; s0 += 2 * CHUNK) {
+        chunk(0, s0, 0);
+        if (s0 + CHUNK >= end) break;
+        chunk(1, s0 + CHUNK, 1);
     }
-    mx4_finish<T, MT, CT, WC>(p, reinterpret_cast<float *>(lds), acc, row0, col0, rows, split, ahead);
+    mx4_finish<T, MT, CT, WC>(p, reinterpret_cast<float *>(lds), acc, row0, col0, rows, split, Mx4First{});
 }
 
 }  // namespace nmspmm
