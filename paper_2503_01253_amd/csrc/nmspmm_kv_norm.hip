@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "nmspmm_kv4.h"
 #include "nmspmm_kv_host.h"
@@ -23,188 +24,279 @@ struct NormArgs {
     const int32_t *seq, *pos;
     const float *cos, *sin, *q_norm, *k_norm;
     int64_t tokens, positions, sequences, table_positions;
-    int32_t heads, rows, dim, rot, interleaved, log_team;
+    int64_t first_token;
+    int32_t heads, q_heads, dim, rot, interleaved, log_team;
+    int32_t slices[3];      // waves that share a group of tokens: for its keys, values and queries
     float eps;
+    double inv_dim;
 };
+
+// How a row is read: value by value; in whole 16-byte pieces; and so also the
+// pieces that turn with them, and the angles.
+enum NormMode { AN_SINGLE, AN_ROWS, AN_WHOLE };
 
 constexpr int AN_NT = 256, AN_NW = AN_NT / 64;
 
-// What a row is combined with: a lane's eight dimensions, and those that turn
-// with them (`with`), their norm's weights and the angles.
-struct Piece {
-    float x[8], with[8], w[8], w_with[8], c[8], s[8];   // s with the sign of with's term
-};
-
-// y = norm, then rotation, of a lane's piece.  F: the type to compute in.
-template <class F>
-__device__ __forceinline__ void norm_and_turn(const Piece &a, F (&y)[8], bool norm, bool rotate, int log_team, int dim,
-                                              float eps)
+// The sum of x over a team of 1 << log_team lanes, in every one of them.
+__device__ __forceinline__ double team_sum(double x, int log_team)
 {
-    F inv = 1;
-    if (norm) {     // the sum in fp64: squares of large fp32 values stay finite
-        double sum = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fma((double)a.x[i], (double)a.x[i], sum);
-        for (int step = 1; step < 1 << log_team; step *= 2) sum += __shfl_xor(sum, step);
-        inv = (F)(1 / sqrt(sum / dim + (double)eps));
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        F own = a.x[i], with = a.with[i];
-        if (norm) {
-            own *= inv * (F)a.w[i];
-            with *= inv * (F)a.w_with[i];
-        }
-        if (!rotate) y[i] = own;
-        else if constexpr (__is_same(F, double)) y[i] = fma(own, (double)a.c[i], with * (double)a.s[i]);
-        else y[i] = fmaf(own, a.c[i], with * a.s[i]);
-    }
+    auto dpp = [](double v, auto ctrl) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        constexpr int C = decltype(ctrl)::value;
+        const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)u, C, 0xf, 0xf, false);
+        const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), C, 0xf, 0xf, false);
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    };
+    x += dpp(x, std::integral_constant<int, 0xb1>{});                           // lane ^ 1
+    x += dpp(x, std::integral_constant<int, 0x4e>{});                           // lane ^ 2
+    if (log_team >= 3) x += dpp(x, std::integral_constant<int, 0x141>{});       // the other four of eight
+    if (log_team >= 4) x += dpp(x, std::integral_constant<int, 0x140>{});       // the other eight of sixteen
+    if (log_team >= 5) x += __shfl_xor(x, 16);
+    if (log_team >= 6) x += __shfl_xor(x, 32);
+    return x;
 }
 
-// A wave takes one row (a key, value or query head) of 64 >> log_team tokens: a
-// team of 1 << log_team lanes a token, eight dimensions a lane, so that a norm's
-// sum and a group's largest magnitude are found between lanes.  A dimension's
-// partner in the rotation is loaded beside it (from the same lines).  VEC: rows
-// and angles in whole 16-byte pieces.  C: the cache's type, or Fp4.
-template <class T, class C, bool VEC>
+// 1 / sqrt(m) in fp64 from the instruction's estimate (23 bits) and `steps` of
+// Newton's iteration, each of which doubles them.
+template <int STEPS>
+__device__ __forceinline__ double inverse_root(double m)
+{
+    const double first = __builtin_amdgcn_rsq(m);
+    double y = first;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) y = fma(0.5 * y, fma(-m * y, y, 1.0), y);
+    return m > 0 && m < __builtin_inf() ? y : first;
+}
+
+// A lane's eight dimensions of a row, and those that turn with them.
+template <class T>
+struct RowPiece {
+    alignas(8 * sizeof(T) < 16 ? 8 * sizeof(T) : 16) T x[8], with[8];
+};
+
+// A wave takes one token and ROWS times 64 >> log_team heads of its keys, its
+// values or its queries: a team of 1 << log_team lanes a head, eight dimensions a
+// lane, so that a norm's sum and a group's largest magnitude are found between
+// lanes.  The place and the angles are found once for all of them, and all heads
+// are loaded before anything is waited for.  The dimensions that turn with a
+// lane's come from another lane (WHOLE), or are loaded beside them.  C: the
+// cache's type, or Fp4: then the keys are computed in fp64, where the weights'
+// products with the angles are exact, and get the codes of the formula.
+//
+// Bound by memory, and for few tokens by the chain pos -> table -> store: 4001
+// tokens of 48 rows of 128 (32 queries, 8 keys and values), both norms, rotation
+// of all dimensions: fp32 into bf16 39 us, 4.6 TB/s; bf16 into bf16 29 us, 3.4
+// TB/s; bf16 into 4 bits 35 us.  64 tokens take 4.1 us.  A wave with four tokens
+// and one head of them took 50, 44 and 50 us, one that goes over many heads in a
+// loop 44, 37 and 40 (it waits for its stores).
+template <class T, class C, NormMode MODE, int ROWS>
 __global__ __launch_bounds__(AN_NT) void nm_append_norm_kernel(NormArgs p)
 {
-    constexpr bool FP4 = __is_same(C, Fp4);
+    constexpr bool FP4 = __is_same(C, Fp4), VEC = MODE != AN_SINGLE, WHOLE = MODE == AN_WHOLE;
     const int lane = threadIdx.x & 63, sub = lane & ((1 << p.log_team) - 1);
-    const int row = blockIdx.y * AN_NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (row >= p.rows) return;
-    const int64_t t = (int64_t)blockIdx.x * (64 >> p.log_team) + (lane >> p.log_team);
-    bool there = t < p.tokens;
-    const bool is_k = row < p.heads, is_v = !is_k && row < 2 * p.heads;
-    const int head = is_k ? row : is_v ? row - p.heads : row - 2 * p.heads;
-    const float *weight = is_k ? p.k_norm : is_v ? nullptr : p.q_norm;
+    const uint32_t wave = blockIdx.x * AN_NW + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t per_group = p.slices[0] + p.slices[1] + p.slices[2], group = wave / per_group;
+    int slice = (int)(wave - group * per_group);
+    const bool is_k = slice < p.slices[0], is_v = !is_k && slice < p.slices[0] + p.slices[1], is_q = !is_k && !is_v;
+    slice -= is_k ? 0 : is_v ? p.slices[0] : p.slices[0] + p.slices[1];
+    const int per = 64 >> p.log_team, begin = slice * ROWS * per + (lane >> p.log_team), heads = is_q ? p.q_heads : p.heads;
+    const int64_t t = p.first_token + group;
+    if (t >= p.tokens) return;
     const int d0 = sub * 8, valid = p.dim - d0 < 0 ? 0 : p.dim - d0 < 8 ? p.dim - d0 : 8;
     const int half = p.rot / 2;
     const bool rotate = !is_v && p.rot > 0;
-
-    Piece a;
-    const int64_t pos = there ? p.pos[t] : -1, seq = there ? p.seq[t] : -1;
-    const T *src = is_k ? static_cast<const T *>(p.k_new) + t * p.kn[0] + head * p.kn[1]
-                 : is_v ? static_cast<const T *>(p.v_new) + t * p.vn[0] + head * p.vn[1]
-                        : static_cast<const T *>(p.q) + t * p.qn[0] + head * p.qn[1];
-    load_row<8, VEC>(src + d0, there ? valid : 0, a.x);
-    if (weight) load_row<8, VEC>(weight + d0, valid, a.w);
-    // the partners: of a pair (d, d + half) in other lanes, of (2d, 2d + 1) in this one
+    const float *w = is_k ? p.k_norm : is_v ? nullptr : p.q_norm;
+    // partners: of a pair (d, d + half) in other lanes, of (2d, 2d + 1) in this one
     const bool apart = rotate && !p.interleaved;
-    if (apart) {
-        if constexpr (VEC) {
-            const int at = d0 < half ? d0 + half : d0 < p.rot ? d0 - half : d0;
-            load_row<8, true>(src + at, there ? valid : 0, a.with);
-            if (weight) load_row<8, true>(weight + at, valid, a.w_with);
-        } else {
+    // (lanes past the row read its start, and their values are not used)
+    const int from = valid > 0 ? d0 : 0, other = !apart || from >= p.rot ? from : from < half ? from + half : from - half;
+
+    auto partner = [&](int d) { return d < half ? d + half : d < p.rot ? d - half : d; };
+    const T *src = is_k ? static_cast<const T *>(p.k_new) + t * p.kn[0]
+                 : is_v ? static_cast<const T *>(p.v_new) + t * p.vn[0]
+                        : static_cast<const T *>(p.q) + t * p.qn[0];
+    const int64_t head_stride = is_k ? p.kn[1] : is_v ? p.vn[1] : p.qn[1];
+    RowPiece<T> rows[ROWS];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int d = d0 + i, at = d < half ? d + half : d < p.rot ? d - half : d;
-                a.with[i] = there && i < valid ? to_f32(src[at]) : 0.f;
-                a.w_with[i] = weight && i < valid ? weight[at] : 0.f;
-            }
-        }
-    } else {
+    for (int r = 0; r < ROWS; ++r) {
+        RowPiece<T> &a = rows[r];
+        const T *row = src + (begin + r * per < heads ? begin + r * per : heads - 1) * head_stride;
+        if constexpr (VEC) __builtin_memcpy(a.x, __builtin_assume_aligned(row + from, 16), sizeof(a.x));
+        else
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            a.with[i] = a.x[i ^ 1];
-            if (weight) a.w_with[i] = a.w[i ^ 1];
-        }
+            for (int i = 0; i < 8; ++i) a.x[i] = i < valid ? row[d0 + i] : T(0);
+        if constexpr (!WHOLE)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a.with[i] = apart && i < valid ? row[partner(d0 + i)] : T(0);
     }
+    const int64_t pos = p.pos[t], seq = p.seq[t];
+    if (pos < 0 || pos >= p.table_positions || seq < 0 || seq >= p.sequences || (p.rot && pos >= p.positions)) return;
+    const Place at = place_of(p.c, p.c.table + seq * p.c.table_stride, (int)pos);
+    if (!at.held) return;
 
-    there = there && pos >= 0 && pos < p.table_positions && seq >= 0 && seq < p.sequences &&
-            !(p.rot && pos >= p.positions);
-    Place at{0, 0, false};
-    if (there) at = place_of(p.c, p.c.table + seq * p.c.table_stride, (int)pos);
-    there = there && at.held;
-
-    if (rotate) {
-        const int64_t angles = (there ? pos : 0) * half;
+    auto finish = [&](auto in) {
+        using F = decltype(in);
+        // y = x * f + with * g: the norm's weights times cos and sin; with and g are
+        // zero where nothing turns (and g -0, which leaves x's sign if x is zero)
+        F f[8], g[8];
+        if (w || rotate) {
+            float c[8], s[8], u[8], v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a.c[i] = 1.f, a.s[i] = 0.f;
-        if constexpr (VEC) {
-            if (there && d0 < p.rot) {
-                if (apart) {
+            for (int i = 0; i < 8; ++i) c[i] = u[i] = v[i] = 1.f, s[i] = 0.f;
+            if (rotate && d0 < p.rot) {
+                const int64_t angles = pos * half;
+                if (WHOLE && apart) {
                     const int e = d0 < half ? d0 : d0 - half;
-                    load_row<8, true>(p.cos + angles + e, 8, a.c);
-                    load_row<8, true>(p.sin + angles + e, 8, a.s);
-                } else {
-                    float c[4], s[4];
-                    load_row<4, true>(p.cos + angles + d0 / 2, 4, c);
-                    load_row<4, true>(p.sin + angles + d0 / 2, 4, s);
+                    load_row<8, true>(p.cos + angles + e, 8, c);
+                    load_row<8, true>(p.sin + angles + e, 8, s);
+                } else if (WHOLE) {
+                    float c4[4], s4[4];
+                    load_row<4, true>(p.cos + angles + d0 / 2, 4, c4);
+                    load_row<4, true>(p.sin + angles + d0 / 2, 4, s4);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) a.c[i] = c[i / 2], a.s[i] = s[i / 2];
+                    for (int i = 0; i < 8; ++i) c[i] = c4[i / 2], s[i] = s4[i / 2];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int d = d0 + i, e = apart ? (d < half ? d : d - half) : d / 2;
+                        if (d < p.rot) c[i] = p.cos[angles + e], s[i] = p.sin[angles + e];
+                    }
                 }
             }
-        } else {
+            if (w) {
+                if (WHOLE) {
+                    load_row<8, true>(w + from, 8, u);
+                    load_row<8, true>(w + other, 8, v);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        u[i] = i < valid ? w[d0 + i] : 0.f;
+                        v[i] = i < valid && apart ? w[partner(d0 + i)] : 0.f;
+                    }
+                }
+                if (!apart)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = u[i ^ 1];
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int d = d0 + i;
-                if (there && d < p.rot) {
-                    const int e = apart ? (d < half ? d : d - half) : d / 2;
-                    a.c[i] = p.cos[angles + e];
-                    a.s[i] = p.sin[angles + e];
-                }
+                const bool minus = apart ? d0 + i < half : i % 2 == 0;
+                f[i] = (F)c[i] * (F)u[i];
+                g[i] = rotate && d0 + i < p.rot ? (F)(minus ? -s[i] : s[i]) * (F)v[i] : F(-0.0);
             }
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (apart ? d0 + i < half : i % 2 == 0) a.s[i] = -a.s[i];
-    }
 
-    float y[8];
-    if (FP4 && is_k && (weight || rotate)) {
-        double z[8];
-        norm_and_turn<double>(a, z, weight != nullptr, rotate, p.log_team, p.dim, p.eps);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = mx4_narrow(z[i]);
-    } else {
-        norm_and_turn<float>(a, y, weight != nullptr, rotate, p.log_team, p.dim, p.eps);
-    }
+        for (int r = 0; r < ROWS; ++r) {
+            const int head = begin + r * per;
+            const bool there = head < heads;
+            RowPiece<T> &a = rows[r];
+            if constexpr (WHOLE) {
+                if (apart) {
+                    int u[sizeof(a.x) / 4];
+                    __builtin_memcpy(u, a.x, sizeof(a.x));
+#pragma unroll
+                    for (int &word : u) word = __builtin_amdgcn_ds_bpermute(4 * lane + (other - from) / 2, word);
+                    __builtin_memcpy(a.with, u, sizeof(u));
+                }
+            }
+            float y[8];
+            if (!w && !rotate) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = to_f32(a.x[i]);
+            } else {
+                float with[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) with[i] = apart ? to_f32(a.with[i]) : to_f32(a.x[i ^ 1]);
+                if (p.rot < p.dim)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) with[i] = d0 + i < p.rot ? with[i] : 0;
+                F inv = 1;
+                if (w) {
+                    double mean = 0;    // in fp64: squares of large fp32 values stay finite
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const double x = to_f32(a.x[i]);
+                        mean = fma(x, x, mean);
+                    }
+                    mean = team_sum(valid > 0 ? mean : 0, p.log_team) * p.inv_dim + (double)p.eps;
+                    inv = inverse_root<__is_same(F, double) ? 2 : 1>(mean);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float x = to_f32(a.x[i]);
+                    if constexpr (__is_same(F, double)) y[i] = mx4_narrow(inv * fma((double)x, f[i], with[i] * g[i]));
+                    else y[i] = fmaf(x * inv, f[i], with[i] * inv * g[i]);
+                }
+            }
 
-    if (!is_k && !is_v) {
-        if (there) store_row<8, VEC>(static_cast<T *>(p.q_out) + t * p.qo[0] + head * p.qo[1] + d0, valid, y);
-        return;
-    }
-    if constexpr (FP4) {
-        uint32_t top = 0;
+            if (is_q) {
+                if (there) store_row<8, VEC>(static_cast<T *>(p.q_out) + t * p.qo[0] + head * p.qo[1] + d0, valid, y);
+                continue;
+            }
+            if constexpr (FP4) {
+                uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (i >= valid) y[i] = 0.f;
-            top = max(top, __builtin_bit_cast(uint32_t, y[i]) & 0x7fffffffu);
+                for (int i = 0; i < 8; ++i) {
+                    if (i >= valid) y[i] = 0.f;
+                    top = max(top, __builtin_bit_cast(uint32_t, y[i]) & 0x7fffffffu);
+                }
+                top = max(top, (uint32_t)__shfl_xor((int)top, 1));      // the four lanes of a group
+                top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+                const uint32_t scale = mx4_scale_of(top), codes = mx4_codes(y, scale);
+                if (there && sub < 4 * p.f.l.G) {
+                    unsigned char *b = p.f.block(at.page, head);
+                    *reinterpret_cast<uint32_t *>(b + (is_k ? p.f.l.k_word(at.slot, sub) : p.f.l.v_word(at.slot, sub))) = codes;
+                    if (sub % 4 == 0)
+                        b[is_k ? p.f.l.k_scale(at.slot, sub / 4) : p.f.l.v_scale(at.slot, sub / 4)] = (unsigned char)scale;
+                }
+            } else if (there) {
+                C *dst = is_k ? static_cast<C *>(p.k_pages) + at.page * p.c.ks[0] + at.slot * p.c.ks[1] + head * p.c.ks[2]
+                              : static_cast<C *>(p.v_pages) + at.page * p.c.vs[0] + at.slot * p.c.vs[1] + head * p.c.vs[2];
+                store_row<8, VEC>(dst + d0, valid, y);
+            }
         }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 1));      // the four lanes of a group
-        top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-        const uint32_t scale = mx4_scale_of(top), codes = mx4_codes(y, scale);
-        if (there && sub < 4 * p.f.l.G) {
-            unsigned char *b = p.f.block(at.page, head);
-            *reinterpret_cast<uint32_t *>(b + (is_k ? p.f.l.k_word(at.slot, sub) : p.f.l.v_word(at.slot, sub))) = codes;
-            if (sub % 4 == 0)
-                b[is_k ? p.f.l.k_scale(at.slot, sub / 4) : p.f.l.v_scale(at.slot, sub / 4)] = (unsigned char)scale;
-        }
-    } else if (there) {
-        C *dst = is_k ? static_cast<C *>(p.k_pages) + at.page * p.c.ks[0] + at.slot * p.c.ks[1] + head * p.c.ks[2]
-                      : static_cast<C *>(p.v_pages) + at.page * p.c.vs[0] + at.slot * p.c.vs[1] + head * p.c.vs[2];
-        store_row<8, VEC>(dst + d0, valid, y);
-    }
+    };
+    if (FP4 && is_k) finish(0.0);
+    else finish(0.f);
 }
 
-template <class T, class C>
-hipError_t launch_norm_to(const NormArgs &p, bool vec, hipStream_t stream)
+template <class T, class C, NormMode MODE, int ROWS>
+hipError_t launch_norm_rows(NormArgs p, hipStream_t stream)
 {
-    const int64_t per = 64 >> p.log_team;
-    const dim3 grid((unsigned)((p.tokens + per - 1) / per), (unsigned)((p.rows + AN_NW - 1) / AN_NW));
-    if (vec) hipLaunchKernelGGL((nm_append_norm_kernel<T, C, true>), grid, dim3(AN_NT), 0, stream, p);
-    else hipLaunchKernelGGL((nm_append_norm_kernel<T, C, false>), grid, dim3(AN_NT), 0, stream, p);
+    const int rows = ROWS * (64 >> p.log_team);
+    p.slices[0] = p.slices[1] = (p.heads + rows - 1) / rows;
+    p.slices[2] = (p.q_heads + rows - 1) / rows;
+    const int64_t slices = 2 * (int64_t)p.slices[0] + p.slices[2];
+    const int64_t most = ((int64_t)1 << 25) / slices;       // (a grid takes fewer than 2^32 threads)
+    for (; p.first_token < p.tokens; p.first_token += most) {
+        const int64_t groups = std::min(most, p.tokens - p.first_token);
+        const dim3 grid((unsigned)((groups * slices + AN_NW - 1) / AN_NW));
+        hipLaunchKernelGGL((nm_append_norm_kernel<T, C, MODE, ROWS>), grid, dim3(AN_NT), 0, stream, p);
+    }
     return hipGetLastError();
 }
 
-template <class T>
-hipError_t launch_norm(const NormArgs &p, bool four, nmspmm_dtype_t cache, bool vec, hipStream_t stream)
+template <class T, class C>
+hipError_t launch_norm_to(const NormArgs &p, NormMode mode, hipStream_t stream)
 {
-    if (four) return launch_norm_to<T, Fp4>(p, vec, stream);
-    if (cache == NMSPMM_F32) return launch_norm_to<T, float>(p, vec, stream);
-    return cache == NMSPMM_BF16 ? launch_norm_to<T, bf16_t>(p, vec, stream) : launch_norm_to<T, f16_t>(p, vec, stream);
+    // two steps of heads a wave where that still fills the card (512 tokens of 48 rows of
+    // 128 into 4 bits: 8.4 us with one, 9.0 with two; 4001 tokens: 41 and 35)
+    const bool many = (p.tokens << p.log_team) / 64 * (2 * (int64_t)p.heads + p.q_heads) >= 8192;
+    if (mode == AN_WHOLE)
+        return many ? launch_norm_rows<T, C, AN_WHOLE, 2>(p, stream) : launch_norm_rows<T, C, AN_WHOLE, 1>(p, stream);
+    if (mode == AN_ROWS)
+        return many ? launch_norm_rows<T, C, AN_ROWS, 2>(p, stream) : launch_norm_rows<T, C, AN_ROWS, 1>(p, stream);
+    return launch_norm_rows<T, C, AN_SINGLE, 1>(p, stream);
+}
+
+template <class T>
+hipError_t launch_norm(const NormArgs &p, bool four, nmspmm_dtype_t cache, NormMode mode,
+                       hipStream_t stream)
+{
+    if (four) return launch_norm_to<T, Fp4>(p, mode, stream);
+    if (cache == NMSPMM_F32) return launch_norm_to<T, float>(p, mode, stream);
+    return cache == NMSPMM_BF16 ? launch_norm_to<T, bf16_t>(p, mode, stream) : launch_norm_to<T, f16_t>(p, mode, stream);
 }
 
 // What the two entry points share.  cache: sizes and table; four: the 4-bit
@@ -251,7 +343,7 @@ nmspmm_status_t append_new(const nmspmm_kv_cache_t *cache, const nmspmm_kv4_cach
                            hipStream_t stream)
 {
     const int64_t rows = 2 * (int64_t)cache->heads + (n.q_heads > INT31 ? INT31 : n.q_heads);
-    // a launch takes fewer than 2^32 threads along x and 2^16 workgroups along y
+    // the sizes of nmspmm_kv_append
     if (n.tokens >= (int64_t)1 << 24 || rows >= (int64_t)1 << 17 || n.positions > INT31) return NMSPMM_ERR_UNSUPPORTED;
     NormArgs p{};
     p.c = device_view(cache);
@@ -279,25 +371,26 @@ nmspmm_status_t append_new(const nmspmm_kv_cache_t *cache, const nmspmm_kv4_cach
     p.sequences = cache->sequences;
     p.table_positions = table_positions(cache);
     p.heads = cache->heads;
-    p.rows = (int)rows;
+    p.q_heads = (int)n.q_heads;
     p.dim = cache->dim;
     p.rot = n.rot;
     p.interleaved = n.interleaved != 0;
     p.eps = n.eps;
+    p.inv_dim = 1.0 / cache->dim;
     for (p.log_team = 2; 8 << p.log_team < cache->dim;) ++p.log_team;
     const int es = dtype_bytes(n.dtype), cs = dtype_bytes(cache->dtype);
-    const bool vec = cache->dim % 8 == 0 && (n.interleaved ? n.rot % 8 == 0 : n.rot % 16 == 0) &&
-                     rows_aligned(n.k, n.ks, 2, cache->dim, es) && rows_aligned(n.v, n.vs, 2, cache->dim, es) &&
-                     aligned_to(n.cos, 16) && aligned_to(n.sin, 16) && aligned_to(n.q_norm, 16) &&
-                     aligned_to(n.k_norm, 16) &&
+    const bool whole = (n.interleaved ? n.rot % 8 == 0 : n.rot % 16 == 0) && aligned_to(n.cos, 16) && aligned_to(n.sin, 16);
+    const bool vec = cache->dim % 8 == 0 && rows_aligned(n.k, n.ks, 2, cache->dim, es) &&
+                     rows_aligned(n.v, n.vs, 2, cache->dim, es) && aligned_to(n.q_norm, 16) && aligned_to(n.k_norm, 16) &&
                      (n.q_heads == 0 || (rows_aligned(n.q, n.qs, 2, cache->dim, es) &&
                                          rows_aligned(n.q_out, n.qos, 2, cache->dim, es))) &&
                      (four || (rows_aligned(cache->k_pages, cache->k_stride, 3, cache->dim, cs) &&
                                rows_aligned(cache->v_pages, cache->v_stride, 3, cache->dim, cs)));
+    const NormMode mode = !vec ? AN_SINGLE : whole ? AN_WHOLE : AN_ROWS;
     const bool f = four != nullptr;
-    const hipError_t e = n.dtype == NMSPMM_F32    ? launch_norm<float>(p, f, cache->dtype, vec, stream)
-                         : n.dtype == NMSPMM_BF16 ? launch_norm<bf16_t>(p, f, cache->dtype, vec, stream)
-                                                  : launch_norm<f16_t>(p, f, cache->dtype, vec, stream);
+    const hipError_t e = n.dtype == NMSPMM_F32    ? launch_norm<float>(p, f, cache->dtype, mode, stream)
+                         : n.dtype == NMSPMM_BF16 ? launch_norm<bf16_t>(p, f, cache->dtype, mode, stream)
+                                                  : launch_norm<f16_t>(p, f, cache->dtype, mode, stream);
     return e == hipSuccess ? NMSPMM_OK : NMSPMM_ERR_HIP;
 }
 

@@ -66,7 +66,7 @@ def declare(L):
     L.nmspmm_mx4_run.restype = I
     L.nmspmm_kv4_page_bytes.argtypes = [I64, I64, I64]
     L.nmspmm_kv4_page_bytes.restype = I64
-    L.nmspmm_kv4_append.argtypes = [C, P, S, P, S, I, I64, P, P, P, P, I64, I, I, P, P, F, P, S, P, S, I64, P]
+    L.nmspmm_kv4_append.argtypes = [C, P, P, P, P, I, I64, P, P, P, P, I64, I, I, P, P, F, P, P, P, P, I64, P]
     L.nmspmm_kv4_append.restype = I
     L.nmspmm_kv4_read.argtypes = [C, I64, P, P, I, P, S, P, S, P]
     L.nmspmm_kv4_read.restype = I
@@ -296,25 +296,47 @@ def nmspmm_kv4_read(cache: Kv4Cache, seq, pos, k_out=None, v_out=None, stream=No
     (k_out, v_out)."""
     import torch
     L = _lib or _library()
+    some = v_out if k_out is None else k_out
+    # as in nmspmm_half_run: one expression, and _check_read words the rest
+    try:
+        at, tokens = cache.at, seq.shape
+        good = (type(cache) is Kv4Cache and seq.dtype is torch.int32 and pos.dtype is torch.int32
+                and seq.get_device() == at and pos.get_device() == at and len(tokens) == 1 and pos.shape == tokens
+                and seq.stride(0) == 1 and pos.stride(0) == 1)
+        dtype, ks, vs = torch.float32, (0, 0), (0, 0)
+        if some is not None:
+            dtype, shape = some.dtype, (tokens[0], cache.heads, cache.dim)
+            good = good and dtype in _dtypes
+        if k_out is not None:
+            ks = k_out.stride()
+            good = good and k_out.shape == shape and k_out.get_device() == at and ks[2] == 1
+        if v_out is not None:
+            vs = v_out.stride()
+            good = good and v_out.shape == shape and v_out.dtype is dtype and v_out.get_device() == at and vs[2] == 1
+    except (AttributeError, IndexError):
+        good = False
+    if not good:
+        _check_read(cache, seq, pos, k_out, v_out)
+    st = _call(torch, at, L.nmspmm_kv4_read, cache._ref, tokens[0], seq.data_ptr(), pos.data_ptr(), _dtypes[dtype],
+               0 if k_out is None else k_out.data_ptr(), _Pair(ks[0], ks[1]), 0 if v_out is None else v_out.data_ptr(),
+               _Pair(vs[0], vs[1]), _raw_stream(torch, at, stream))
+    if st:
+        _check("nmspmm_kv4_read", st)
+    return k_out, v_out
+
+
+def _check_read(cache, seq, pos, k_out, v_out):
+    import torch
     _check_cache(cache, Kv4Cache)
     _require("seq", seq, (torch.int32,), 1, cache.device)
     _require("pos", pos, (torch.int32,), 1, cache.device)
     _shape("pos", pos, seq.shape)
-    outs, dtype = [], None
+    dtypes = tuple(_dtypes)
     for name, t in (("k_out", k_out), ("v_out", v_out)):
-        if t is None:
-            outs += [None, None]
-            continue
-        _require(name, t, tuple(_dtypes) if dtype is None else (dtype,), 3, cache.device)
-        _shape(name, t, (seq.shape[0], cache.heads, cache.dim))
-        dtype = t.dtype
-        outs += [t.data_ptr(), _Pair(t.stride(0), t.stride(1))]
-    at = cache.at
-    st = _call(torch, at, L.nmspmm_kv4_read, cache._ref, seq.shape[0], seq.data_ptr(), pos.data_ptr(),
-               _dtypes[dtype or torch.float32], *outs, _raw_stream(torch, at, stream))
-    if st:
-        _check("nmspmm_kv4_read", st)
-    return k_out, v_out
+        if t is not None:
+            _require(name, t, dtypes, 3, cache.device)
+            _shape(name, t, (seq.shape[0], cache.heads, cache.dim))
+            dtypes = (t.dtype,)
 
 
 def nmspmm_kv4_attend_workspace_bytes(cache: Kv4Cache, q_heads: int, max_length: int, window: int = 0) -> int:

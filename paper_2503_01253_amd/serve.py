@@ -37,6 +37,7 @@ class _Cache(ctypes.Structure):
 
 
 _Pair = ctypes.c_int64 * 2
+_Strides = ctypes.c_int64 * 8
 _lib = None
 _dtypes = None
 
@@ -70,7 +71,8 @@ def declare(L):
     L.nmspmm_half_run.restype = I
     L.nmspmm_kv_append.argtypes = [C, P, S, P, S, I, I64, P, P, P, P, I64, I, I, P, S, P, S, I64, P]
     L.nmspmm_kv_append.restype = I
-    L.nmspmm_kv_append_norm.argtypes = [C, P, S, P, S, I, I64, P, P, P, P, I64, I, I, P, P, F, P, S, P, S, I64, P]
+    # (strides as addresses: four in one array of _append_norm's)
+    L.nmspmm_kv_append_norm.argtypes = [C, P, P, P, P, I, I64, P, P, P, P, I64, I, I, P, P, F, P, P, P, P, I64, P]
     L.nmspmm_kv_append_norm.restype = I
     L.nmspmm_kv_attend_workspace_bytes.argtypes = [C, I64, I64, I64]
     L.nmspmm_kv_attend_workspace_bytes.restype = I64
@@ -352,60 +354,70 @@ def _append_norm(name, call, kind, cache, k, v, seq, pos, cos, sin, q, q_out, in
         raise ValueError("q_out without q")
     if q is not None and q_out is None:
         q_out = q
-    angles, queries = (None, None, 0, 0), (None, None, None, None, 0)
     # as in nmspmm_half_run: one expression each, and the _check_ functions word the rest
     try:
-        at, dtype, shape, ks, vs = cache.at, k.dtype, k.shape, k.stride(), v.stride()
+        at, dtype, shape, ks, vs, dim = cache.at, k.dtype, k.shape, k.stride(), v.stride(), cache.dim
+        tokens = shape[:1]
         good = (type(cache) is kind and dtype in _dtypes and v.dtype is dtype and k.get_device() == at
-                and v.get_device() == at and len(shape) == 3 and v.shape == shape and shape[1] == cache.heads
-                and shape[2] == cache.dim and ks[2] == 1 and vs[2] == 1 and seq.dtype is torch.int32
-                and pos.dtype is torch.int32 and seq.get_device() == at and pos.get_device() == at
-                and seq.shape == shape[:1] and pos.shape == seq.shape and seq.stride(0) == 1 and pos.stride(0) == 1)
-    except AttributeError:
+                and v.get_device() == at and v.shape == shape and shape[1:] == (cache.heads, dim)
+                and ks[2] == 1 and vs[2] == 1 and seq.dtype is torch.int32 and pos.dtype is torch.int32
+                and seq.get_device() == at and pos.get_device() == at and seq.shape == tokens
+                and pos.shape == tokens and seq.stride(0) == 1 and pos.stride(0) == 1)
+    except (AttributeError, IndexError):
         good = False
     if not good:
         _check_append(cache, k, v, seq, pos, kind)
+    cosp = sinp = rows = rot = 0
     if cos is not None:
         try:
+            angles = cos.shape
             good = (cos.dtype is torch.float32 and sin.dtype is torch.float32 and cos.get_device() == at
-                    and sin.get_device() == at and cos.dim() == 2 and sin.shape == cos.shape and cos.is_contiguous()
+                    and sin.get_device() == at and len(angles) == 2 and sin.shape == angles and cos.is_contiguous()
                     and sin.is_contiguous())
         except AttributeError:
             good = False
         if not good:
             _check_angles(cache, cos, sin)
-        rows, half = cos.shape
-        angles = (cos.data_ptr(), sin.data_ptr(), rows, 2 * half)
+        rows, rot = angles[0], 2 * angles[1]
+        cosp, sinp = cos.data_ptr(), sin.data_ptr()
+    qp = qop = heads = 0
+    qs = qos = (0, 0)
     if q is not None:
         try:
             heads, qs, qos = q.shape[1], q.stride(), q_out.stride()
             good = (q.dtype is dtype and q_out.dtype is dtype and q.get_device() == at and q_out.get_device() == at
-                    and q.shape == (shape[0], heads, cache.dim) and q_out.shape == q.shape and qs[2] == 1
+                    and q.shape == (shape[0], heads, dim) and q_out.shape == q.shape and qs[2] == 1
                     and qos[2] == 1)
         except (AttributeError, IndexError):
             good = False
         if not good:
             _check_queries(cache, k, q, q_out)
-        queries = (q.data_ptr(), _Pair(qs[0], qs[1]), q_out.data_ptr(), _Pair(qos[0], qos[1]), heads)
-    norms = []
-    for word, w in (("q_norm", q_norm), ("k_norm", k_norm)):
-        if w is None:
-            norms.append(None)
-            continue
-        try:
-            good = (w.dtype is torch.float32 and w.get_device() == at and w.shape == (cache.dim,) and w.stride(0) == 1)
-        except AttributeError:
-            good = False
-        if not good:
-            _require(word, w, (torch.float32,), 1, cache.device)
-            _shape(word, w, (cache.dim,))
-        norms.append(w.data_ptr())
-    st = _call(torch, at, call, cache._ref, k.data_ptr(), _Pair(ks[0], ks[1]), v.data_ptr(), _Pair(vs[0], vs[1]),
-               _dtypes[dtype], shape[0], seq.data_ptr(), pos.data_ptr(), *angles, interleaved, *norms, eps, *queries,
-               _raw_stream(torch, at, stream))
+        qp, qop = q.data_ptr(), q_out.data_ptr()
+    qn = kn = 0
+    if q_norm is not None:
+        qn = _norm_weight("q_norm", q_norm, cache, torch)
+    if k_norm is not None:
+        kn = _norm_weight("k_norm", k_norm, cache, torch)
+    strides = _Strides(ks[0], ks[1], vs[0], vs[1], qs[0], qs[1], qos[0], qos[1])
+    here = ctypes.addressof(strides)
+    st = _call(torch, at, call, cache._ref, k.data_ptr(), here, v.data_ptr(), here + 16, _dtypes[dtype], shape[0],
+               seq.data_ptr(), pos.data_ptr(), cosp, sinp, rows, rot, interleaved, qn, kn, eps, qp, here + 32, qop,
+               here + 48, heads, _raw_stream(torch, at, stream))
     if st:
         _check(name, st)
     return q_out
+
+
+def _norm_weight(name, w, cache, torch):
+    """The address of a norm's weights."""
+    try:
+        good = w.dtype is torch.float32 and w.get_device() == cache.at and w.shape == (cache.dim,) and w.stride(0) == 1
+    except AttributeError:
+        good = False
+    if not good:
+        _require(name, w, (torch.float32,), 1, cache.device)
+        _shape(name, w, (cache.dim,))
+    return w.data_ptr()
 
 
 def _check_cache(cache, kind=None):
