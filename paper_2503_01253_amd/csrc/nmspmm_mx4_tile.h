@@ -558,6 +558,15 @@ __global__ __launch_bounds__(MX4_NT, 2) void nm_mx4_wide_kernel(Mx4Args p)
                 }
             }
     };
+    // NaN in the places this thread's stores will fill
+    auto poison_a = [&](int slot) {
+#pragma unroll
+        for (int i = 0; i < NB * 8; ++i) {
+            const int c = (kc0 + i / 8 * KB) * 8 + i % 8;
+            *reinterpret_cast<u32x2 *>(lds + slot * SLOT + c * PITCH + (((rb >> 2) ^ swizzle(c)) << 5) + 8 * (rb & 3)) =
+                u32x2{~0u, ~0u};
+        }
+    };
 
     f32x4 acc[CT][MT];
 #pragma unroll
@@ -598,6 +607,7 @@ __global__ __launch_bounds__(MX4_NT, 2) void nm_mx4_wide_kernel(Mx4Args p)
     auto chunk = [&](int d, int s0, int slot) {
         store_a(d, slot);
         lds_sync();
+        if constexpr (NMSPMM_POISON_LDS) poison_a(slot ^ 1);    // (free, as above)
         const int64_t c0 = mx4_chunk_base(p, s0);
 #pragma unroll
         for (int i = 0; i < D; ++i) {
