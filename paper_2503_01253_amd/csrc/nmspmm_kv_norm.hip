@@ -268,7 +268,9 @@ hipError_t launch_norm_rows(NormArgs p, hipStream_t stream)
     p.slices[0] = p.slices[1] = (p.heads + rows - 1) / rows;
     p.slices[2] = (p.q_heads + rows - 1) / rows;
     const int64_t slices = 2 * (int64_t)p.slices[0] + p.slices[2];
-    const int64_t most = ((int64_t)1 << 25) / slices;       // (a grid takes fewer than 2^32 threads)
+    // a grid takes fewer than 2^32 threads, and all but the last end with their waves: a
+    // query that is turned in place is read once
+    const int64_t most = ((int64_t)1 << 25) / slices / AN_NW * AN_NW;
     for (; p.first_token < p.tokens; p.first_token += most) {
         const int64_t groups = std::min(most, p.tokens - p.first_token);
         const dim3 grid((unsigned)((groups * slices + AN_NW - 1) / AN_NW));
