@@ -370,31 +370,21 @@ void launch_join(const AttendArgs &p, int64_t rows, hipStream_t stream)
 }
 
 AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window, bool mfma,
-                       bool split, int64_t groups, int64_t most)
+                       bool split)
 {
     const int64_t group = q_heads / c->heads;
-<<<<<<< Updated upstream
     const int GT = mfma ? ATTEND_MFMA_HEADS : group >= 5 ? 8 : group >= 3 ? 4 : (int)group;
     const int64_t span = attend_span(c, max_length, window);
     const int64_t base = c->sequences * c->heads * ((group + GT - 1) / GT);
     // eight workgroups a CU (two or three run at once), each of 256 positions at
     // least; and of 1024 at most, for batches whose lengths differ, which only
-=======
-    a.GT = mfma ? ATTEND_MFMA_HEADS : group >= 5 ? 8 : group >= 3 ? 4 : (int)group;
-    a.gtiles = (int)((group + a.GT - 1) / a.GT);
-    int64_t span = std::min({max_length, table_positions(c), KV_MAX_LENGTH});
-    if (window > 0) span = std::min(span, window);
-    const int64_t base = c->sequences * c->heads * a.gtiles;
-    // (groups = 2048) eight workgroups a CU (two or three run at once), each of 256 positions at
-    // least; and (most) of 1024 at most, for batches whose lengths differ, which only
->>>>>>> Stashed changes
     // the device knows (192 sequences of 0 to 5000 positions, 64 heads on 8: 273
     // us, with chunks of 2500 404; 64 of 8192 each: 420 and 407), up to 64
     // workgroups a CU (which bounds the workspace)
     int64_t splits = 1;
     if (split && base > 0) {
-        splits = std::max<int64_t>(1, std::min<int64_t>((groups + base - 1) / base, span / 256));
-        splits = std::max(splits, std::min<int64_t>({JN_SPLITS, (span + most - 1) / most, 16384 / base}));
+        splits = std::max<int64_t>(1, std::min<int64_t>((JN_SPLITS + base - 1) / base, span / 256));
+        splits = std::max(splits, std::min<int64_t>({JN_SPLITS, (span + 1023) / 1024, 16384 / base}));
     }
     return attend_cut(c, q_heads, span, GT, splits);
 }

@@ -252,7 +252,6 @@ bool attend4_takes_mfma(const nmspmm_kv4_cache_t *c)
     return c->page_size % 4 == 0 && c->dim <= 256 && kv4_layout(c->page_size, c->dim).block < (int64_t)1 << 31;
 }
 
-<<<<<<< Updated upstream
 // How the work is cut.  For the matrix-core kernel, of which a CU holds four
 // workgroups: into what runs at once, where that leaves chunks of 256 to 2048
 // positions (one sequence of 131071 on 8 heads 37.5 us, in twice as many chunks 43);
@@ -277,15 +276,6 @@ AttendPlan attend4_plan(const nmspmm_kv4_cache_t *c, int64_t q_heads, int64_t ma
         }
     }
     return attend_cut(&sizes, q_heads, span, ATTEND_MFMA_HEADS, splits);
-=======
-// How the work is cut: for the matrix-core kernel, of which four workgroups run on a
-// CU, all of them at once, and chunks twice the 16-bit cache's.
-AttendPlan attend4_plan(const nmspmm_kv4_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window, bool split)
-{
-    const nmspmm_kv_cache_t sizes = kv4_sizes(c);
-    const bool mfma = attend4_takes_mfma(c);
-    return attend_plan(&sizes, q_heads, max_length, window, mfma, split, getenv("T1") ? atoi(getenv("T1")) : mfma ? 1024 : 2048, getenv("T3") ? atoi(getenv("T3")) : mfma ? 2048 : 1024);
->>>>>>> Stashed changes
 }
 
 nmspmm_status_t check_attend4_sizes(const nmspmm_kv4_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window)

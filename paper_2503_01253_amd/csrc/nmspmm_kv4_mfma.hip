@@ -98,7 +98,6 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
     // that it takes of each: with few groups, 16 / (4 DK) lanes share a word's codes
     constexpr int VU = DK == 8 ? 2 : 1, SHARE = DK == 1 ? 4 : DK == 2 ? 2 : 1, NI = 8 / SHARE, LD = 16 / SHARE;
     constexpr int NT = VU * NI, AP = DK * 32 + 4, SW = DK > 4 ? 2 : 1;
-    constexpr int R = DK > 4 && QP > 1 ? 1 : 2;     // tiles on their way
     __shared__ __align__(16) float acc[A4M_NW * GT * AP];
     __shared__ float2 s_ml[A4M_NW][GT];
     // A sequence's chunks start at one that differs from sequence to sequence: in the
@@ -136,7 +135,6 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
         }
         return w;
     };
-<<<<<<< Updated upstream
     // (selections, no branches: what is selected is there)
     const uint32_t pages = (uint32_t)p.c.pages;
     auto held = [&](int32_t page) { return (uint32_t)page < pages; };
@@ -198,12 +196,6 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
     uint32_t kw[2][DK], ks[2][SW], vs[2][VU];
     u32x4 vw[2][VU];
     auto load_k = [&](const Where &w) {
-=======
-    uint32_t rk[R][2][DK], rks[R][2][SW], rvs[R][2][VU];
-    u32x4 rv[R][2][VU];
-    auto load_k = [&](int r, const Where &w) {
-        uint32_t (&kw)[2][DK] = rk[r], (&ks)[2][SW] = rks[r];
->>>>>>> Stashed changes
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const unsigned char *at = place(w, s, false, 0, 16 * G, k_mine);
@@ -221,9 +213,7 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
             else __builtin_memcpy(ks[s], __builtin_assume_aligned(sc, 4 * SW), 4 * SW);
         }
     };
-    auto load_v = [&](int r, const Where &w) {
-        u32x4 (&vw)[2][VU] = rv[r];
-        uint32_t (&vs)[2][VU] = rvs[r];
+    auto load_v = [&](const Where &w) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -267,7 +257,6 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
 
     int base = (t.begin & ~(A4M_TOKENS - 1)) + wave * A4M_TOKENS;
     constexpr int STEP = A4M_NW * A4M_TOKENS;
-<<<<<<< Updated upstream
     Where cur, next;        // of the tile that is in the registers, and of the one after it
     if (base < end) {
         cur = p.window > 0 ? look_up(base) : first;
@@ -277,22 +266,6 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
     }
     load_q();
     for (; base < end; base += STEP) {
-=======
-    Where now[R], next[R];      // of the tile that is in the registers, and of the one after it there
-#pragma unroll
-    for (int r = 0; r < R; ++r) now[r] = look_up(base + r * STEP);
-#pragma unroll
-    for (int r = 0; r < R; ++r) next[r] = look_up(base + (R + r) * STEP);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        load_k(r, now[r]);
-        load_v(r, now[r]);
-    }
-    auto tile = [&](int r, int base) {
-        uint32_t (&kw)[2][DK] = rk[r], (&ks)[2][SW] = rks[r], (&vs)[2][VU] = rvs[r];
-        u32x4 (&vw)[2][VU] = rv[r];
-        const Where &cur = now[r];
->>>>>>> Stashed changes
         f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
         auto group = [&](auto index) {
             constexpr int c = decltype(index)::value;
@@ -314,7 +287,7 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
         group(std::integral_constant<int, 5>{});
         group(std::integral_constant<int, 6>{});
         group(std::integral_constant<int, 7>{});
-        load_k(r, next[r]);
+        load_k(next);
         float x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = s[j / 4][j % 4] * p.scale2;
@@ -388,14 +361,9 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
             byte(std::integral_constant<int, 2>{}, u);
             byte(std::integral_constant<int, 3>{}, u);
         }
-        load_v(r, next[r]);
-        now[r] = next[r];
-        next[r] = look_up(base + 2 * R * STEP);
-    };
-    for (; base < t.end; base += R * STEP) {
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (base + r * STEP < t.end) tile(r, base + r * STEP);
+        load_v(next);
+        cur = next;
+        next = look_up(base + 2 * STEP);
     }
 
     // ---- the four waves joined ----

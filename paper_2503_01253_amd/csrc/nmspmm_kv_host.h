@@ -72,10 +72,8 @@ struct AttendPlan {
     int64_t ml_bytes, bytes;    // workspace
 };
 
-// nmspmm_kv.hip.  mfma: tiles of 16 query heads; split: sequences may be cut, into chunks
-// that make about `groups` workgroups and have at most `most` positions.
+// nmspmm_kv.hip.  mfma: tiles of 16 query heads; split: sequences may be cut.
 AttendPlan attend_plan(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window, bool mfma,
-<<<<<<< Updated upstream
                        bool split);
 
 // The positions of a sequence that a call may attend to, at most.
@@ -102,9 +100,6 @@ inline AttendPlan attend_cut(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_
     return a;
 }
 
-=======
-                       bool split, int64_t groups = 2048, int64_t most = 1024);
->>>>>>> Stashed changes
 nmspmm_status_t check_attend_sizes(const nmspmm_kv_cache_t *c, int64_t q_heads, int64_t max_length, int64_t window);
 constexpr int JN_SPLITS = 2048;     // most chunks of a sequence
 void launch_join(const AttendArgs &p, int64_t rows, hipStream_t stream);     // the parts of split sequences joined
