@@ -302,7 +302,7 @@ def nmspmm_kv4_read(cache: Kv4Cache, seq, pos, k_out=None, v_out=None, stream=No
         at, tokens = cache.at, seq.shape
         good = (type(cache) is Kv4Cache and seq.dtype is torch.int32 and pos.dtype is torch.int32
                 and seq.get_device() == at and pos.get_device() == at and len(tokens) == 1 and pos.shape == tokens
-                and seq.stride(0) == 1 and pos.stride(0) == 1)
+                and seq.is_contiguous() and pos.is_contiguous())
         dtype, ks, vs = torch.float32, (0, 0), (0, 0)
         if some is not None:
             dtype, shape = some.dtype, (tokens[0], cache.heads, cache.dim)

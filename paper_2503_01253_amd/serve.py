@@ -362,7 +362,7 @@ def _append_norm(name, call, kind, cache, k, v, seq, pos, cos, sin, q, q_out, in
                 and v.get_device() == at and v.shape == shape and shape[1:] == (cache.heads, dim)
                 and ks[2] == 1 and vs[2] == 1 and seq.dtype is torch.int32 and pos.dtype is torch.int32
                 and seq.get_device() == at and pos.get_device() == at and seq.shape == tokens
-                and pos.shape == tokens and seq.stride(0) == 1 and pos.stride(0) == 1)
+                and pos.shape == tokens and seq.is_contiguous() and pos.is_contiguous())
     except (AttributeError, IndexError):
         good = False
     if not good:
@@ -411,7 +411,7 @@ def _append_norm(name, call, kind, cache, k, v, seq, pos, cos, sin, q, q_out, in
 def _norm_weight(name, w, cache, torch):
     """The address of a norm's weights."""
     try:
-        good = w.dtype is torch.float32 and w.get_device() == cache.at and w.shape == (cache.dim,) and w.stride(0) == 1
+        good = w.dtype is torch.float32 and w.get_device() == cache.at and w.shape == (cache.dim,) and w.is_contiguous()
     except AttributeError:
         good = False
     if not good:
