@@ -74,8 +74,8 @@ NMSPMM_API int64_t nmspmm_mx4_workspace_bytes(int64_t m, const nmspmm_mx4_weight
  * Products of A's values and the weight's are exact in fp32; sums, epilogue
  * and (where k is split) partial sums are fp32; C is rounded once (ties to
  * even).  The order of summation is fixed by shape, alignment and workspace.  Only kept
- * rows of B enter a sum.  Made for the few rows of decoding: from about 64
- * rows on a 16-bit weight and nmspmm_half_run do better.  m == 0 or n == 0
+ * rows of B enter a sum.  Made for the few rows of decoding: from about 32
+ * rows on nmspmm_half_run on a 16-bit weight is as fast or faster.  m == 0 or n == 0
  * returns NMSPMM_OK without a launch; with k == 0 the sum is zero.  Errors: as
  * for nmspmm_half_run. */
 NMSPMM_API nmspmm_status_t nmspmm_mx4_run(const void *A, int64_t lda, nmspmm_dtype_t a_dtype,

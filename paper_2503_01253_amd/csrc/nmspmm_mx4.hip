@@ -176,24 +176,31 @@ struct Mx4GeneralArgs {
     int64_t lda, m, n;
     int N, M, V;
     HalfEpilogue epi;
+    int64_t first;      // column of the launch
 };
 
-constexpr int MG_ROWS = 8;
+constexpr int MG_ROWS = 8, MG_COLS = 32, MG_SLICES = 8;
 
-// Any shape: a thread owns one column and MG_ROWS rows of C and walks the
-// compressed rows; bound by the loads of A, one value per multiply-add.
+// Any shape: a thread owns one column, MG_ROWS rows of C and a slice of the
+// compressed rows, which it walks; the slices' sums are added in order.  Bound by
+// the loads of A, one value per multiply-add (8 x 4096 x 4096 at 16:32, V = 8: 222
+// us; one thread for all of k, 256 columns a workgroup: 1377).
 template <class T, class O>
-__global__ __launch_bounds__(256) void nm_mx4_general_kernel(Mx4GeneralArgs p)
+__global__ __launch_bounds__(MG_COLS * MG_SLICES) void nm_mx4_general_kernel(Mx4GeneralArgs p)
 {
-    const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (j >= p.n) return;
+    __shared__ float part[MG_SLICES][MG_ROWS][MG_COLS];
+    const int col = threadIdx.x % MG_COLS, slice = threadIdx.x / MG_COLS;
+    const int64_t j = p.first + (int64_t)blockIdx.x * MG_COLS + col;
+    const bool mine = j < p.n;
     const T *A = static_cast<const T *>(p.A);
     const unsigned char *scales = p.packed + p.l.scales_at;
     const unsigned char *offs = p.N == p.M ? nullptr : p.packed + p.l.offs_at + j / p.V;
+    const int64_t rows = (p.l.groups + MG_SLICES - 1) / MG_SLICES * 32;
+    const int64_t begin = slice * rows, end = begin + rows < p.l.w ? begin + rows : p.l.w;
     for (int64_t i0 = (int64_t)blockIdx.y * MG_ROWS; i0 < p.m; i0 += (int64_t)gridDim.y * MG_ROWS) {
         float sum[MG_ROWS] = {};
-        int64_t window = 0;
-        for (int64_t u = 0, r = 0; u < p.l.w; ++u) {
+        int64_t window = begin / p.N * p.M, r = begin % p.N;
+        for (int64_t u = begin; mine && u < end; ++u) {
             const uint32_t code = p.packed[u / 2 * p.n + j] >> (u % 2 * 4) & 15u;
             const float s = mx4_scale<0>(scales[u / 32 * p.n + j]);
             const float b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, s, 0)[0];
@@ -207,18 +214,29 @@ __global__ __launch_bounds__(256) void nm_mx4_general_kernel(Mx4GeneralArgs p)
             }
         }
 #pragma unroll
-        for (int i = 0; i < MG_ROWS; ++i)
-            if (i0 + i < p.m) half_store<O>(p.epi, i0 + i, j, sum[i]);
+        for (int i = 0; i < MG_ROWS; ++i) part[slice][i][col] = sum[i];
+        __syncthreads();
+        // a row a slice's threads
+        float all = 0.f;
+#pragma unroll
+        for (int x = 0; x < MG_SLICES; ++x) all += part[x][slice][col];
+        if (mine && i0 + slice < p.m) half_store<O>(p.epi, i0 + slice, j, all);
+        __syncthreads();
     }
 }
 
 template <class T>
-hipError_t launch_general(const Mx4GeneralArgs &p, hipStream_t stream)
+hipError_t launch_general(Mx4GeneralArgs p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((p.n + 255) / 256),
-                    (unsigned)std::min<int64_t>(65535, (p.m + MG_ROWS - 1) / MG_ROWS));
-    if (p.epi.f32) hipLaunchKernelGGL((nm_mx4_general_kernel<T, float>), grid, dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((nm_mx4_general_kernel<T, T>), grid, dim3(256), 0, stream, p);
+    static_assert(MG_ROWS == MG_SLICES, "a row a slice's threads");
+    const int64_t most = (int64_t)1 << 28;      // (a grid takes fewer than 2^32 threads)
+    for (; p.first < p.n; p.first += most) {
+        const dim3 grid((unsigned)((std::min(most, p.n - p.first) + MG_COLS - 1) / MG_COLS),
+                        (unsigned)std::min<int64_t>(65535, (p.m + MG_ROWS - 1) / MG_ROWS));
+        const dim3 block(MG_COLS * MG_SLICES);
+        if (p.epi.f32) hipLaunchKernelGGL((nm_mx4_general_kernel<T, float>), grid, block, 0, stream, p);
+        else hipLaunchKernelGGL((nm_mx4_general_kernel<T, T>), grid, block, 0, stream, p);
+    }
     return hipGetLastError();
 }
 
@@ -537,7 +555,7 @@ extern "C" nmspmm_status_t nmspmm_mx4_run(const void *A, int64_t lda, nmspmm_dty
     }
     hipError_t e;
     if (c.general) {
-        const Mx4GeneralArgs p{A, static_cast<const unsigned char *>(w.packed), l, lda, m, w.n, w.N, w.M, w.V, epi};
+        const Mx4GeneralArgs p{A, static_cast<const unsigned char *>(w.packed), l, lda, m, w.n, w.N, w.M, w.V, epi, 0};
         e = a_dtype == NMSPMM_BF16 ? launch_general<bf16_t>(p, stream) : launch_general<f16_t>(p, stream);
     } else {
         e = a_dtype == NMSPMM_BF16 ? run_tiles<bf16_t>(c, l, A, lda, w, m, epi, workspace, stream)
