@@ -21,7 +21,7 @@
  * The library's only global state is the static scratch array of
  * nmspmm_run_noalloc (with its per-device address) and a table of at most 16
  * cached workspaces of nmspmm_run, nmspmm_run_ex and the calls of
- * nmspmm_serve.h, one per (device, stream), allocated on first use and kept
+ * nmspmm_serve.h and nmspmm_mx4.h, one per (device, stream), allocated on first use and kept
  * until the process ends; it is safe to call from several host threads.
  */
 #ifndef NMSPMM_H
