@@ -211,7 +211,7 @@ __global__ __launch_bounds__(AN_NT) void nm_append_norm_kernel(NormArgs p)
                 if (p.rot < p.dim)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) with[i] = d0 + i < p.rot ? with[i] : 0;
-                F inv = 1;
+                double inv = 1;
                 if (w) {
                     double mean = 0;    // in fp64: squares of large fp32 values stay finite
 #pragma unroll
@@ -222,11 +222,18 @@ __global__ __launch_bounds__(AN_NT) void nm_append_norm_kernel(NormArgs p)
                     mean = team_sum(valid > 0 ? mean : 0, p.log_team) * p.inv_dim + (double)p.eps;
                     inv = inverse_root<__is_same(F, double) ? 2 : 1>(mean);
                 }
+                // (in fp64 too where fp32 does not hold the factor: rows of tiny or huge values)
+                const bool far = !(inv >= 0x1p-120 && inv <= 0x1p120);
+                if (__is_same(F, double) || __any(far)) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float x = to_f32(a.x[i]);
-                    if constexpr (__is_same(F, double)) y[i] = mx4_narrow(inv * fma((double)x, f[i], with[i] * g[i]));
-                    else y[i] = fmaf(x * inv, f[i], with[i] * inv * g[i]);
+                    for (int i = 0; i < 8; ++i) {
+                        const double z = inv * fma((double)to_f32(a.x[i]), (double)f[i], (double)with[i] * (double)g[i]);
+                        y[i] = __is_same(F, double) ? mx4_narrow(z) : (float)z;
+                    }
+                } else {
+                    const float inv32 = (float)inv;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = fmaf(to_f32(a.x[i]) * inv32, (float)f[i], with[i] * inv32 * (float)g[i]);
                 }
             }
 
