@@ -166,7 +166,8 @@ NMSPMM_API nmspmm_status_t nmspmm_kv_append(const nmspmm_kv_cache_t *cache, cons
  *   x[d] * weight[d] / sqrt(mean(x^2) + eps)     over its dim dimensions
  *   q_norm, k_norm   dim fp32 weights, or NULL: no norm of the queries or keys
  * Norm (its sum fp64) and rotation are fp32, and a value is rounded once, after
- * both.  All else as in nmspmm_kv_append, but for the sizes it refuses: 2^24 tokens or
+ * both; what has no norm is as nmspmm_kv_append writes it, to the bit.  All else as
+ * there, but for the sizes it refuses: 2^24 tokens or
  * more, 2^17 heads or more, keys, values and queries together.  Errors: as there, and
  * NMSPMM_ERR_INVALID_ARG for an eps that is negative or NaN,
  * NMSPMM_ERR_UNSUPPORTED for misaligned weights. */

@@ -65,6 +65,17 @@ __device__ __forceinline__ void turn_pair(float &a, float &b, float c, float s)
     b = y;
 }
 
+// The first (or the second) of a pair alone, rounded as turn_pair rounds it.
+// s: minus the sine for the first.
+__device__ __forceinline__ float turn_one(float own, float other, float c, float s, bool second)
+{
+    float y = second ? fmaf(other, s, own * c) : fmaf(own, c, other * s);
+#ifdef __HIP_DEVICE_COMPILE__
+    asm("" : "+v"(y));
+#endif
+    return y;
+}
+
 constexpr float NEG_INF = -__builtin_inff();
 
 // The reference a running maximum stands for: scores are taken relative to

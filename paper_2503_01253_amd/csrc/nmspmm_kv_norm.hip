@@ -134,6 +134,7 @@ __global__ __launch_bounds__(AN_NT) void nm_append_norm_kernel(NormArgs p)
     const Place at = place_of(p.c, p.c.table + seq * p.c.table_stride, (int)pos);
     if (!at.held) return;
 
+    auto first = [&](int i) { return apart ? d0 + i < half : i % 2 == 0; };     // of its pair
     auto finish = [&](auto in) {
         using F = decltype(in);
         // y = x * f + with * g: the norm's weights times cos and sin; with and g are
@@ -180,9 +181,8 @@ __global__ __launch_bounds__(AN_NT) void nm_append_norm_kernel(NormArgs p)
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool minus = apart ? d0 + i < half : i % 2 == 0;
                 f[i] = (F)c[i] * (F)u[i];
-                g[i] = rotate && d0 + i < p.rot ? (F)(minus ? -s[i] : s[i]) * (F)v[i] : F(-0.0);
+                g[i] = rotate && d0 + i < p.rot ? (F)(first(i) ? -s[i] : s[i]) * (F)v[i] : F(-0.0);
             }
         }
 
@@ -230,6 +230,10 @@ __global__ __launch_bounds__(AN_NT) void nm_append_norm_kernel(NormArgs p)
                         const double z = inv * fma((double)to_f32(a.x[i]), (double)f[i], (double)with[i] * (double)g[i]);
                         y[i] = __is_same(F, double) ? mx4_narrow(z) : (float)z;
                     }
+                } else if (!w) {        // as nmspmm_kv_append rounds
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        y[i] = turn_one(to_f32(a.x[i]), with[i], (float)f[i], (float)g[i], !first(i));
                 } else {
                     const float inv32 = (float)inv;
 #pragma unroll
