@@ -222,9 +222,10 @@ __global__ __launch_bounds__(AN_NT) void nm_append_norm_kernel(NormArgs p)
                     mean = team_sum(valid > 0 ? mean : 0, p.log_team) * p.inv_dim + (double)p.eps;
                     inv = inverse_root<__is_same(F, double) ? 2 : 1>(mean);
                 }
-                // (in fp64 too where fp32 does not hold the factor: rows of tiny or huge values)
+                // (in fp64 too where fp32 does not hold the factor: rows of tiny or huge values;
+                // by a team's own, so that a head's bits do not depend on its neighbours)
                 const bool far = !(inv >= 0x1p-120 && inv <= 0x1p120);
-                if (__is_same(F, double) || __any(far)) {
+                if (__is_same(F, double) || far) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const double z = inv * fma((double)to_f32(a.x[i]), (double)f[i], (double)with[i] * (double)g[i]);
