@@ -147,7 +147,8 @@ NMSPMM_API int64_t nmspmm_kv4_attend_workspace_bytes(const nmspmm_kv4_cache_t *c
                                           int64_t max_length, int64_t window);
 
 /* Attention of one new token per sequence over the 4-bit cache: arguments,
- * results and what is left out as in nmspmm_kv_attend.  Scores, softmax and
+ * results and what is left out as in nmspmm_kv_attend (an infinite query as an
+ * infinity in the range there).  Scores, softmax and
  * sums are fp32; queries and weights of the softmax enter the products with
  * all their bits (in bf16 parts), the cache's values as they are. */
 NMSPMM_API nmspmm_status_t nmspmm_kv4_attend(const nmspmm_kv4_cache_t *cache, const void *q, const int64_t *q_stride,

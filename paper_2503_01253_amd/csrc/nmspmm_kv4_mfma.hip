@@ -244,8 +244,9 @@ __global__ __launch_bounds__(A4M_NT, DK > 4 && QP > 2 ? 1 : DK > 4 || QP > 1 ? 2
             for (int j = 0; j < 8; ++j) {
                 short part[QP];
                 split_parts<QP>(x[j], part);
+                const bool whole = fabsf(x[j]) == -NEG_INF;     // (of an infinity a difference leaves NaN)
 #pragma unroll
-                for (int i = 0; i < QP; ++i) q[i][c][j] = part[i];
+                for (int i = 0; i < QP; ++i) q[i][c][j] = i > 0 && whole ? (short)0 : part[i];
             }
         }
     };
