@@ -410,6 +410,13 @@ __global__ __launch_bounds__(MX4_NT, LDS <= 80 * 1024 ? 4 : 2) void nm_mx4_spars
                                 (uint32_t)((row * p.lda + c0) * 2 + at + lane * 16));
             }
         } else {
+            if constexpr (NMSPMM_POISON_LDS) {      // (as lds_dma does)
+                for (int row = wave; row < rows; row += MX4_NW)
+                    for (int c = lane; c < cols; c += 64)
+                        *reinterpret_cast<uint16_t *>(dst + row * p.pitch + c * 2) = (uint16_t)~0u;
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));  // lgkmcnt(0)
+            }
             for (int row = wave; row < rows; row += MX4_NW)
                 for (int c = lane; c < cols; c += 64)
                     *reinterpret_cast<T *>(dst + row * p.pitch + c * 2) = A[row * p.lda + c0 + c];
