@@ -30,8 +30,8 @@ struct Mx4Args {
     int64_t lda, m, n, k, first_row;
     int32_t w, N, M, V;
     int32_t steps;              // groups (dense: steps of four) of all of k
-    int32_t splits, per_split;  // slices of k (neighbouring workgroups: a slice's are on one XCD, which
-                                // reads its part of A once), and the steps of one
+    int32_t splits, per_split;  // slices of k, for more than 16 rows (neighbouring workgroups: a slice's
+                                // are on one XCD, which reads its part of A once), and the steps of one
     int32_t tiles;              // runs of CT column tiles (dense: column tiles)
     int32_t rows;               // rows of a workgroup, 16 MT at most
     int32_t chunk;              // sparse: groups of a chunk of A (a multiple of WK)
@@ -41,8 +41,6 @@ struct Mx4Args {
 };
 
 constexpr int MX4_NW = 8, MX4_NT = 64 * MX4_NW;
-
-
 
 template <class T>
 __device__ __forceinline__ s16x8 mx4_operand(uint32_t w, float scale)
@@ -141,12 +139,12 @@ struct Mx4First {
 };
 
 template <class T, int COLS>
-__device__ __forceinline__ Mx4First mx4_first(const Mx4Args &p, int64_t row0, int64_t col0, int rows, bool split)
+__device__ __forceinline__ Mx4First mx4_first(const Mx4Args &p, int64_t row0, int64_t col0, int rows)
 {
     Mx4First a{0.f, 1.f, 0.f};
     const int row = threadIdx.x / COLS;
     const int64_t r = row0 + row, j = col0 + threadIdx.x % COLS;
-    if (split || row >= rows || j >= p.n) return a;
+    if (row >= rows || j >= p.n) return a;
     if (p.epi.bias) a.bias = p.epi.bias[j];
     if (p.epi.mul) {
         const int64_t at = r * p.epi.ld_mul + j;
@@ -173,7 +171,7 @@ __device__ __forceinline__ void mx4_store(const HalfEpilogue &e, int64_t i, int6
 }
 
 // The sums of the WK waves that share columns, added in their order, and the
-// epilogue (or, with k in slices, the slice's partial sums).  Wave wk * WC + wc holds
+// epilogue (or, with k in slices, the slice's partial sums: more than 16 rows only).  Wave wk * WC + wc holds
 // columns wc * CT * 16 and on; red holds MX4_NW * CT * MT * 256 floats.  Up to 16 rows
 // one output a thread, more than 16 four columns, MX4_U times at once (64 x 4096 at k =
 // 512 one after another 15 us, so 8.4; 1 x 4096 x 11008, dense, 7.2 and so 9.2).
@@ -193,7 +191,6 @@ __device__ __forceinline__ void mx4_finish(const Mx4Args &p, float *red, const f
 #pragma unroll
             for (int e = 0; e < 4; ++e) red[(((wave * CT + c) * MT + t) * 4 + e) * 64 + lane] = acc[c][t][e];
     lds_sync();
-    const int64_t part = split ? ((int64_t)(blockIdx.x % p.splits) * p.m + row0) * p.n : 0;
     if constexpr (MT == 1) {
         for (int i = tid; i < rows * COLS; i += MX4_NT) {
             const int row = i / COLS, col = i % COLS;
@@ -203,14 +200,14 @@ __device__ __forceinline__ void mx4_finish(const Mx4Args &p, float *red, const f
             for (int k = 0; k < WK; ++k) sum += x[k * (WC * CT * 256)];
             const int64_t r = row0 + row, j = col0 + col;
             if (j >= p.n) continue;
-            if (split) p.part[part + row * p.n + j] = sum;
-            else if (i == tid) {
+            if (i == tid) {
                 if (p.epi.f32) mx4_store<float>(p.epi, r, j, sum, ahead);
                 else mx4_store<T>(p.epi, r, j, sum, ahead);
             } else if (p.epi.f32) half_store<float>(p.epi, r, j, sum);
             else half_store<T>(p.epi, r, j, sum);
         }
     } else {
+        const int64_t part = split ? ((int64_t)(blockIdx.x % p.splits) * p.m + row0) * p.n : 0;
         for (int first = tid; first < rows * COLS / 4; first += MX4_NT * MX4_U) {
             Mx4Ahead a[MX4_U];
 #pragma unroll
@@ -252,7 +249,8 @@ __global__ __launch_bounds__(MX4_NT, MT == 1 && VEC ? 4 : 2) void nm_mx4_dense_k
     const int col = lane & 15, grp = lane >> 4;
     const int64_t row0 = p.first_row + (int64_t)blockIdx.y * p.rows;
     const int rows = (int)min64(p.rows, p.m - row0);
-    const int column = p.splits > 1 ? blockIdx.x / p.splits : blockIdx.x, slice = blockIdx.x - column * p.splits;
+    const bool split = MT > 1 && p.splits > 1;
+    const int column = split ? blockIdx.x / p.splits : blockIdx.x, slice = split ? blockIdx.x - column * p.splits : 0;
     const int first = slice * p.per_split, last = min(first + p.per_split, p.steps) - 1;
     const unsigned char *vals[CT], *scales[CT];
 #pragma unroll
@@ -265,9 +263,8 @@ __global__ __launch_bounds__(MX4_NT, MT == 1 && VEC ? 4 : 2) void nm_mx4_dense_k
 #pragma unroll
     for (int t = 0; t < MT; ++t) a_row[t] = static_cast<const T *>(p.A) + (row0 + min(t * 16 + col, rows - 1)) * p.lda;
 
-    const bool split = p.splits > 1;
     const int64_t col0 = (int64_t)column * (CT * 16);
-    const Mx4First ahead = MT == 1 ? mx4_first<T, CT * 16>(p, row0, col0, rows, split) : Mx4First{};
+    const Mx4First ahead = MT == 1 ? mx4_first<T, CT * 16>(p, row0, col0, rows) : Mx4First{};
     u32x4 rv[D][CT];
     uint32_t rs[D][CT];
     s16x8 ra[D][4][MT];
@@ -371,17 +368,15 @@ __global__ __launch_bounds__(MX4_NT, LDS <= 80 * 1024 ? 4 : 2) void nm_mx4_spars
     const int col = lane & 15, grp = lane >> 4, wc = wave % WC, wk = wave / WC;
     const int64_t row0 = p.first_row + (int64_t)blockIdx.y * p.rows;
     const int rows = (int)min64(p.rows, p.m - row0);
-    const int column = p.splits > 1 ? blockIdx.x / p.splits : blockIdx.x, slice = blockIdx.x - column * p.splits;
-    const int first = slice * p.per_split, end = min(first + p.per_split, p.steps);
+    const int column = blockIdx.x, end = p.steps;
     const int64_t tile = min(column * WC + wc, p.tiles - 1);
     const unsigned char *vals = p.vals + tile * p.steps * (256 * CT) + lane * (4 * CT);
     const unsigned char *scales = p.scales + tile * p.steps * (16 * SP) + col * SP;
     const unsigned char *offs = reinterpret_cast<const unsigned char *>(p.offs) +
                                 (tile * (CT * 16) / p.V) * p.steps * 64 + grp * 16;
 
-    const bool split = p.splits > 1;
     const int64_t col0 = (int64_t)column * (WC * CT * 16);
-    const Mx4First ahead = mx4_first<T, WC * CT * 16>(p, row0, col0, rows, split);
+    const Mx4First ahead = mx4_first<T, WC * CT * 16>(p, row0, col0, rows);
     uint32_t rv[D][CT], rs[D];
     u32x4 ro[D];
     auto load = [&](int i, int step) {
@@ -443,14 +438,14 @@ __global__ __launch_bounds__(MX4_NT, LDS <= 80 * 1024 ? 4 : 2) void nm_mx4_spars
         for (int c = 0; c < CT; ++c) mx4_group<T, 1>(a, rv[i][c], mx4_scale_at(rs[i], c), acc[c]);
     };
 
-    load_a(first, 0);
+    load_a(0, 0);
 #pragma unroll
-    for (int i = 0; i < D; ++i) load(i, first + wk + i * WK);
+    for (int i = 0; i < D; ++i) load(i, wk + i * WK);
     // every wave takes the same number of groups (the last may be none), so
     // that all meet at the chunks' ends
-    int slot = 1, chunk_end = first;
+    int slot = 1, chunk_end = 0;
     int64_t c0 = 0;
-    for (int s0 = first; s0 < end; s0 += D * WK) {
+    for (int s0 = 0; s0 < end; s0 += D * WK) {
 #pragma unroll
         for (int i = 0; i < D; ++i) {
             const int s = s0 + i * WK;
@@ -466,7 +461,7 @@ __global__ __launch_bounds__(MX4_NT, LDS <= 80 * 1024 ? 4 : 2) void nm_mx4_spars
             load(i, s + wk + D * WK);
         }
     }
-    mx4_finish<T, 1, CT, WC>(p, reinterpret_cast<float *>(lds), acc, row0, col0, rows, split, ahead);
+    mx4_finish<T, 1, CT, WC>(p, reinterpret_cast<float *>(lds), acc, row0, col0, rows, false, ahead);
 }
 
 // Columns of A that a slot of the kernel below holds, and its threads' blocks of A.
