@@ -53,8 +53,10 @@ NMSPMM_API nmspmm_status_t nmspmm_mx4_quantize(const void *Bc, nmspmm_dtype_t bc
                                     uint8_t *codes, uint8_t *scales, hipStream_t stream);
 
 /* Lays a weight out for nmspmm_mx4_run.  codes and scales as
- * nmspmm_mx4_quantize writes them (or from elsewhere: any scale byte; of a
- * code the low four bits count), idx (w x q bytes) as in nmspmm.h, read only.
+ * nmspmm_mx4_quantize writes them (or from elsewhere: any scale byte, but a
+ * value that fp32 does not hold, of the bytes 253 and 254, may count as an
+ * infinity; of a code the low four bits count), idx (w x q bytes) as in
+ * nmspmm.h, read only.
  * weight->packed is written.  An offset >= M is clamped to M-1, as nmspmm_run
  * does; with N = M the offsets are 0 to M-1 and idx is not read (it may be
  * NULL).  Errors: as for nmspmm_half_pack. */
