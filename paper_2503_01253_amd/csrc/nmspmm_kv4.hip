@@ -253,7 +253,8 @@ bool attend4_takes_mfma(const nmspmm_kv4_cache_t *c)
 }
 
 // How the work is cut.  For the matrix-core kernel, of which a CU holds four
-// workgroups: into what runs at once, where that leaves chunks of 256 to 2048
+// workgroups with bf16 queries, pages of 16 and up to 128 dimensions (three to one in
+// its other forms, which are cut alike): into what runs at once, where that leaves chunks of 256 to 2048
 // positions (one sequence of 131071 on 8 heads 37.5 us, in twice as many chunks 43);
 // else into quarters of the longest, 1024 to 2048 positions each, for batches whose
 // lengths differ (48 sequences of 0 to 5000, in chunks of 1792, 1280 and 640: 42.3,

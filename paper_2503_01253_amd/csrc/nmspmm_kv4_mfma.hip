@@ -18,7 +18,7 @@
 // The next tokens' codes are on their way meanwhile, their pages looked up before.
 // The waves are joined in LDS.
 // 128 x 8192 positions, 32 heads on 8 of 128, 218-222 us (5.2 TB/s), one sequence of
-// 131071, 64 heads on 8, 36-37 with its joining (3.9 TB/s).  A tile of 32 tokens takes a
+// 131071, 64 heads on 8, 37-38 with its joining (3.8 TB/s).  A tile of 32 tokens takes a
 // SIMD some 230 vector and 32 matrix instructions, 0.5 us of them alone, and 4.3 KB, 0.2
 // us at the HBM's rate: four waves a SIMD keep enough of them on their way.  Two tiles
 // ahead a wave took the registers of a fourth wave (219 -> 225 us).

@@ -86,7 +86,7 @@ struct RowPiece {
 // Bound by memory, and for few tokens by the chain pos -> table -> store: 4001
 // tokens of 48 rows of 128 (32 queries, 8 keys and values), both norms, rotation
 // of all dimensions: fp32 into bf16 39 us, 4.6 TB/s; bf16 into bf16 29 us, 3.4
-// TB/s; bf16 into 4 bits 35 us.  64 tokens take 4.1 us.  A wave with four tokens
+// TB/s; bf16 into 4 bits 34 us.  64 tokens take 4.5 us.  A wave with four tokens
 // and one head of them took 50, 44 and 50 us, one that goes over many heads in a
 // loop 44, 37 and 40 (it waits for its stores).
 template <class T, class C, NormMode MODE, int ROWS>

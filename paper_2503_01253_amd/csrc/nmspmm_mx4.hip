@@ -244,7 +244,7 @@ hipError_t launch_general(Mx4GeneralArgs p, hipStream_t stream)
 
 // The slices of C added in order, then the epilogue, four columns a thread (n is
 // a multiple of 16 here): eight slices' loads, and those of the epilogue, on their
-// way at once (64 x 4096 from 8 slices and a term 4.7 us; one slice after another 12).
+// way at once (64 x 4096 from 8 slices and a term 3.9 us; one slice after another 12).
 template <class T>
 __global__ __launch_bounds__(128) void nm_mx4_join_kernel(const float *part, int64_t m, int64_t n, int splits,
                                                           HalfEpilogue epi)
@@ -291,7 +291,8 @@ Mx4Plan mx4_plan(int64_t m, const Mx4Layout &l, const nmspmm_mx4_weight_t &w, bo
     if (l.kind == Mx4Kind::Dense) {
         // one workgroup a CU, as far as four tiles each go; more than 16 rows, of which
         // every workgroup reads all of A: four (1 x 4096 x 11008, 688 tiles:
-        // CT = 1 to 4 9.4, 8.7, 7.2 and 7.9 us; 1 x 8192 x 8192, 512 tiles: 13.1, 9.0, 9.9, 11.3)
+        // CT = 1 to 4 9.3, 8.3, 7.0 and 7.9 us; 1 x 8192 x 8192, 512 tiles: 12.0, 9.2, 10.5, 11.5;
+        // 1 x 4096 x 16384, 1024: 12.2, 9.4, 10.5, 9.0)
         c.CT = c.MT > 1 ? 4 : (int)std::min<int64_t>(4, (w.n / 16 + 255) / 256);
     } else {
         c.CT = l.CT;
@@ -309,7 +310,7 @@ Mx4Plan mx4_plan(int64_t m, const Mx4Layout &l, const nmspmm_mx4_weight_t &w, bo
             c.rows = (int)std::min<int64_t>(m, 16);
             // one workgroup a CU, where A's rows may take all of its LDS, as far as four
             // runs of tiles each go (13 x 4096 x 11008 at 8:32, 344 runs: WC = 1, 2 and 4
-            // 11.4, 9.1 and 12.7 us; 1 x 8192 x 8192 at 4:32, 128 runs: 5.5, 6.8, 9.4)
+            // 10.6, 8.1 and 10.7 us; 1 x 8192 x 8192 at 4:32, 128 runs: 4.6, 5.7, 8.0)
             const int64_t runs = w.n / (16 * l.CT);
             c.WC = runs <= 256 ? 1 : runs <= 512 ? 2 : 4;
             c.wide = (runs + c.WC - 1) / c.WC * ((m + c.rows - 1) / c.rows) <= 256;
@@ -336,8 +337,8 @@ Mx4Plan mx4_plan(int64_t m, const Mx4Layout &l, const nmspmm_mx4_weight_t &w, bo
                                                          : (w.n / (16 * c.CT) + c.WC - 1) / c.WC;
         const int64_t tiles = columns * ((m + 16 * c.MT - 1) / (16 * c.MT));
         // k in slices where the tiles leave CUs idle, of eight steps at least (64 x 11008 x
-        // 4096 at 16:32, 32 tiles: 1, 2, 4 and 8 slices 54, 36, 25 and 18 us; 40 x 4096 x
-        // 11008 at 4:32, 86 tiles, 16 steps: 1, 2 and 4 15.4, 14 and 21)
+        // 4096 at 16:32, 32 tiles: 1, 2, 4 and 8 slices 49, 30, 21 and 17 us; 40 x 4096 x
+        // 11008 at 4:32, 86 tiles, 16 steps: 1 and 2 13.9 and 13.1, 4 half as much again)
         c.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / tiles, l.steps / 8, 16}));
     }
     c.per_split = (l.steps + c.splits - 1) / c.splits;

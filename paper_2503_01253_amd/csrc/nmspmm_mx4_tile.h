@@ -239,7 +239,7 @@ __device__ __forceinline__ void mx4_finish(const Mx4Args &p, float *red, const f
 // Dense.  A workgroup owns CT column tiles and 16 MT rows; its eight waves take
 // the steps of (a slice of) k in turn, D of them on their way.  VEC: A's rows
 // start on 16 bytes and k is a multiple of 8.  (1 x 4096 x 11008, CT = 3: D = 2 7.2 us,
-// 3.3 TB/s, D = 3 8.4, D = 4 8.3; 1 x 4096 x 4096, CT = 1: 4.8, 5.6, 5.6.  Lanes of rows
+// 3.3 TB/s, D = 3 8.4, D = 4 8.3; CT = 4 keeps four registers in memory; 1 x 4096 x 4096, CT = 1: 4.8, 5.6, 5.6.  Lanes of rows
 // past the last that load nothing: 7.6 and 5.4, for their branches.)
 template <class T, int MT, int CT, int D, bool VEC>
 __global__ __launch_bounds__(MX4_NT, MT == 1 && VEC ? 4 : 2) void nm_mx4_dense_kernel(Mx4Args p)
