@@ -384,10 +384,14 @@ void launch_tiles(const Mx4Plan &c, Mx4Kind kind, Mx4Args p, hipStream_t stream)
         const dim3 grid((unsigned)((p.tiles + run - 1) / run * c.splits),
                         (unsigned)((std::min(most, p.m - p.first_row) + c.rows - 1) / c.rows));
         if (kind == Mx4Kind::Dense) {
-            if (c.CT == 1) launch_dense<T, MT, 1>(p, grid, stream);
-            else if (c.CT == 2) launch_dense<T, MT, 2>(p, grid, stream);
-            else if (c.CT == 3) launch_dense<T, MT, 3>(p, grid, stream);
-            else launch_dense<T, MT, 4>(p, grid, stream);
+            if constexpr (MT == 1) {
+                if (c.CT == 1) launch_dense<T, 1, 1>(p, grid, stream);
+                else if (c.CT == 2) launch_dense<T, 1, 2>(p, grid, stream);
+                else if (c.CT == 3) launch_dense<T, 1, 3>(p, grid, stream);
+                else launch_dense<T, 1, 4>(p, grid, stream);
+            } else {
+                launch_dense<T, MT, 4>(p, grid, stream);
+            }
         } else {
             if (c.CT == 1) launch_sparse<T, MT, 1>(c, p, grid, stream);
             else if (c.CT == 2) launch_sparse<T, MT, 2>(c, p, grid, stream);
